@@ -327,6 +327,111 @@ int s3_sae_train_step(const float* x, int B, int d_head, int n_feat, int k, floa
                       float lr, float beta1, float beta2, float eps, int step, float* loss_out,
                       int32_t* ids_out, float* grads_out, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * A paged cache of keys and values, what appends to it and what reads it.  The index above names the
+ * evidence of a long context; these calls keep that context's keys and values and attend to all of them
+ * (prefill) or to the blocks that were named (Sec. 3.6: generation from the selected positions).
+ *
+ * The cache is memory of the caller's, in pages of page_size tokens that belong to one sequence each (or to
+ * several that share a prefix, as long as none of them appends to it).  With E = 16 bytes / element size:
+ *   k    [n_pages][n_kv_heads][d_head / E][page_size][E]   dtype
+ *   v    [n_pages][n_kv_heads][page_size / E][d_head][E]   dtype
+ *   sig  [n_pages][n_kv_heads][d_head]                     bf16, or NULL: no signatures
+ * all 256-byte aligned.  A signature stands for the keys of a page in s3_block_select (below).
+ * Limits: dtype S3_BF16 or S3_FP32; d_head in {64, 128, 256}; page_size a power of two, 16 .. 256;
+ * n_pages >= 1; 1 <= n_kv_heads <= 4096.  Nothing in a cache has to be cleared: slots that no sequence has reached yet are
+ * never read, whatever they hold. */
+typedef struct {
+    void* k;
+    void* v;
+    void* sig;
+    int dtype, n_pages, page_size, n_kv_heads, d_head;
+} s3_kv_cache;
+
+/* The sequences of one call, each with some new tokens.  The new tokens of sequence s are rows
+ * q_start[s] .. q_start[s + 1] - 1 of the call's arrays; they are the LAST of its kv_len[s] tokens (new ones
+ * counted), so row i of n stands at position kv_len[s] - n + i.  Position p lies in slot p % page_size of page
+ * block_table[s * table_stride + p / page_size].
+ *   q_start      [n_seq + 1] int32, ascending, q_start[n_seq] <= n_tokens; NULL: one new token per sequence, n_tokens == n_seq
+ *   kv_len       [n_seq] int32;  block_table [n_seq][table_stride] int32, max_pages entries of a row used
+ *   max_new, max_kv   bounds of a sequence's new tokens and of kv_len: they size workspaces and share out the work, and
+ *                what goes beyond them may be left out
+ * Host structs of device pointers; the arrays are read when the kernels run.  What they hold cannot be checked on
+ * the host: tokens past n_tokens are left out, a position whose block is beyond max_pages or whose page number is outside
+ * [0, n_pages) is not stored and is masked for every reader, and rows of no sequence are not written.
+ * Limits: n_seq <= 2^20, n_tokens <= 2^24, max_pages * page_size <= 2^30, kv_len <= 2^30; n_tokens == 0 is a no-op. */
+typedef struct {
+    const int32_t* q_start;
+    const int32_t* kv_len;
+    const int32_t* block_table;
+    int64_t table_stride;
+    int n_seq, n_tokens, max_pages, max_new, max_kv;
+} s3_kv_batch;
+
+/* cos | sin of the rotary embedding, rounded once from 64 bits: table[p][i] = cos(a), table[p][rot_dim / 2 + i] = sin(a) with
+ * a = p * theta^(-2 i / rot_dim), i < rot_dim / 2.  table [n_pos][rot_dim] fp32, 16-byte aligned.  rot_dim a multiple of 16, <= 256;
+ * n_pos >= 0; theta > 0. */
+int s3_rope_table(float* table, int64_t n_pos, int rot_dim, double theta, void* stream);
+
+/* Appends the batch's tokens: keys and values go to their slots, keys rotated on the way, the queries of the same
+ * tokens rotated into q_out, and the signatures of every page that got a token are computed anew.
+ *   k, v, q   [n_tokens][heads][d_head] with any strides in elements that are multiples of 16 bytes (the three may
+ *             be parts of one projection's output); q may be NULL
+ *   rope      [n_pos][rot_dim] fp32 (s3_rope_table) or NULL: nothing is rotated.  The first rot_dim channels are rotated in
+ *             pairs (i, i + rot_dim / 2), or (2 i, 2 i + 1) with interleaved: a' = a cos - b sin, b' = b cos + a sin,
+ *             every product and sum rounded to fp32, the result once to dtype.  rot_dim a multiple of 16, <= d_head.
+ *   positions [n_tokens] int32 or NULL: the table's row for a token, where it is not its position in the sequence
+ *             (kept evidence of a longer context).  Rows outside the table are taken as its first or last.
+ *   q_out     [n_tokens][n_q_heads][d_head], contiguous, dtype
+ * The signature of a page and head: the mean m of the keys stored there (a sequence's last page: of those up to its length),
+ * in fp32 (partial sums over slots of equal remainder mod 8, in ascending order, then (0+1)+(2+3) and (4+5)+(6+7), joined, divided by the number),
+ * rounded to whole multiples of 2^(floor(log2 max|m|) - 6): at most 128 of them, so bf16 holds it exactly.  Zero where max|m|
+ * is not in [2^-40, 2^50).
+ * Limits: n_q_heads a multiple of n_kv_heads where q is given. */
+int s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* k, int64_t k_tok_stride,
+                 int64_t k_head_stride, const void* v, int64_t v_tok_stride, int64_t v_head_stride, const float* rope,
+                 int64_t n_pos, int rot_dim, int interleaved, const int32_t* positions, const void* q, int n_q_heads,
+                 int64_t q_tok_stride, int64_t q_head_stride, void* q_out, void* stream);
+
+/* Attention of the new tokens over everything that their sequences hold, themselves included (append first):
+ *   out[t, h] = sum_j softmax_j(scale q[t, h] . k[j, h / G]) v[j, h / G] over the positions j <= p (t's own), and
+ *   j > p - window where window > 0; G = n_q_heads / n_kv_heads.
+ *   lse[t, h] = log sum_j exp(scale q . k) (natural log), or NULL.
+ * A row that sees nothing (kv_len smaller than the number of new tokens, unmapped pages) is 0 with lse -inf.  Values in masked
+ * places never reach a row, infinities and NaN included.
+ * Softmax statistics and sums in fp32; with bf16 the weights are rounded to bf16 for the second product.
+ *   q    [n_tokens][n_q_heads][d_head], strides as in s3_kv_append;  out [n_tokens][n_q_heads][d_head] contiguous, dtype
+ *   ws   s3_paged_attention_workspace(...) bytes, 256-byte aligned, contents meaningless between calls
+ * Limits: 1 <= G <= 32; scale > 0; window >= 0. */
+size_t s3_paged_attention_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads);
+int s3_paged_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
+                       int64_t q_tok_stride, int64_t q_head_stride, float scale, int window, void* out, float* lse,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/* The blocks (pages) that each tile of queries will read, chosen by the signatures.  A sequence's new tokens are cut into
+ * tiles of q_block (the last may be shorter); tiles are numbered through over the sequences.  For every tile and
+ * key/value head the rows are the tile's tokens times the G query heads; each row is rounded to its own 8 bit grid as a signature is, and
+ *   score(b) = max over rows of  row . sig[page of block b]
+ * (whole multiples of one power of two: exact in fp32 in any order, so the choice is the same everywhere).  Candidates are
+ * the mapped blocks up to that of the tile's last position.  The first `lead` of them, and with tail > 0 those from
+ * tail - 1 before the block of the tile's first position on, are always taken; then the largest scores, ties to the lower block.
+ *   sel [s3_block_tiles(batch, q_block)][n_kv_heads][top_b] int32: the chosen blocks in ascending order, then -1.
+ *   ws  s3_block_select_workspace(...) bytes, 256-byte aligned.
+ * Limits: cache->sig; q_block >= 1; 1 <= top_b <= 4096; lead, tail >= 0; lead + tail + (q_block + page_size - 2) / page_size <= top_b. */
+int64_t s3_block_tiles(const s3_kv_batch* batch, int q_block);
+size_t s3_block_select_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads, int q_block, int top_b);
+int s3_block_select(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
+                    int64_t q_tok_stride, int64_t q_head_stride, int q_block, int top_b, int lead, int tail, int32_t* sel,
+                    void* ws, size_t ws_bytes, void* stream);
+
+/* s3_paged_attention over the positions of listed blocks only: sel as s3_block_select writes it, or made from the
+ * spans of s3_coactivate_score / s3_select_spans.  Entries that are negative, beyond the sequence or unmapped are passed over, in any
+ * place; a block listed twice counts twice.  The causal limit holds inside the listed blocks. */
+size_t s3_block_attention_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads, int q_block, int top_b);
+int s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
+                       int64_t q_tok_stride, int64_t q_head_stride, const int32_t* sel, int q_block, int top_b,
+                       float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif
