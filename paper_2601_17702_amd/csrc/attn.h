@@ -37,11 +37,18 @@ struct AttnArgs {
     int n_kv, G, n_q, window;
     int qb, top, per_q;       // lists: tokens a tile, entries, tiles of 32 rows a tile of queries
     float sl;                 // scale * log2(e)
+    int few;                  // sequences of at most 32 rows are another launch's
 };
 
-// Largest over the two lanes that share a row; their sum.
-__device__ __forceinline__ float kv_pair_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
-__device__ __forceinline__ float kv_pair_sum(float x) { return x + __shfl_xor(x, 32); }
+// Largest over the two lanes that share a row; their sum.  The swap hands every lane both halves' values.
+__device__ __forceinline__ float kv_pair_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float kv_pair_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
 // What a wavefront knows of its 32 rows: row r0 + (lane & 31) of the sequence's n * G, head and token of it.
 template <typename T, int D>
@@ -68,10 +75,72 @@ struct AttnRows {
     }
 };
 
-// Running softmax of a row: m the largest scaled score (log2 units), l this lane's part of the sum, o the products so far:
-// o[dt][i] is channel 32 dt + 8 (i / 4) + 4 half + i % 4.
+// Largest magnitude of a piece's elements as the bits of a float, and at least 0x7f800000 exactly where one is infinite or NaN.
+__device__ __forceinline__ unsigned kv_magnitude(kv_bf16x8 v, unsigned x) {
+    const kv_u32x4 u = __builtin_bit_cast(kv_u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x = max(max(x, u[i] & 0x7fffffffu), u[i] << 16 & 0x7fffffffu);
+    return x;
+}
+__device__ __forceinline__ unsigned kv_magnitude(kv_f32x4 v, unsigned x) {
+    const kv_u32x4 u = __builtin_bit_cast(kv_u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x = max(x, u[i] & 0x7fffffffu);
+    return x;
+}
+// Zero in place of infinities and NaN.
+__device__ __forceinline__ kv_bf16x8 kv_finite(kv_bf16x8 v) {
+    kv_u32x4 u = __builtin_bit_cast(kv_u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        u[i] &= (u[i] & 0x7f800000u) == 0x7f800000u ? 0xffffu : ~0u;
+        u[i] &= (u[i] & 0x7f80u) == 0x7f80u ? 0xffff0000u : ~0u;
+    }
+    return __builtin_bit_cast(kv_bf16x8, u);
+}
+__device__ __forceinline__ kv_f32x4 kv_finite(kv_f32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = fabsf(v[i]) < INFINITY ? v[i] : 0.0f;
+    return v;
+}
+// The first n elements of a piece, zeros behind them (n may be negative or more than there are).
+__device__ __forceinline__ kv_bf16x8 kv_first(kv_bf16x8 v, int n) {
+    kv_u32x4 u = __builtin_bit_cast(kv_u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] &= n > 2 * i + 1 ? 0xffffffffu : n > 2 * i ? 0xffffu : 0u;
+    return __builtin_bit_cast(kv_bf16x8, u);
+}
+__device__ __forceinline__ kv_f32x4 kv_first(kv_f32x4 v, int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = n > i ? v[i] : 0.0f;
+    return v;
+}
+
+// The tokens a row sees, as low <= position <= low + span; position 2^30 is beyond all rows.
+struct AttnSight {
+    int low;
+    unsigned span;
+    __device__ __forceinline__ AttnSight(int pos, int hi, int window) {
+        const int up = min(pos, hi - 1);
+        low = window ? max(0, pos - window + 1) : 0;
+        span = (unsigned)(up - low);
+        if (up < low) {                  // none: no position is -1
+            low = -1;
+            span = 0;
+        }
+    }
+    __device__ __forceinline__ bool sees(int pos) const { return (unsigned)(pos - low) <= span; }
+};
+
+// Running softmax of a row: m the scaled score (log2 units) that its weights are taken against, at most kSlack below the largest so
+// far; l this lane's part of the weights' sum, o the products so far: o[dt][i] is channel 32 dt + 8 (i / 4) + 4 half + i % 4.
+// Rescaling o takes D / 2 instructions per 32 tokens, more than the exponentials: it is done only where a row's largest score has
+// grown by more than kSlack (weights of up to 2^kSlack are as exact as those below 1).
+constexpr float kSlack = 8.0f;
 template <typename T, int D>
 struct AttnState {
+    typedef typename KvElem<T>::vec vec;
+    static constexpr int E = KvElem<T>::E, NW = 16 / E;
     float m, l;
     kv_f32x16 o[D / 32];
     __device__ __forceinline__ void clear() {
@@ -82,26 +151,51 @@ struct AttnState {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
     }
-    // s: raw scores of 32 tokens, -inf where masked.  Leaves the weights in w.
-    __device__ __forceinline__ void softmax(const kv_f32x16& s, float sl, typename KvElem<T>::vec (&w)[16 / KvElem<T>::E]) {
-        constexpr int E = KvElem<T>::E;
-        float x = s[0];
+    // s: raw scores of NS tiles of 32 tokens, -inf where masked.  Leaves the weights in w.
+    template <int NS>
+    __device__ __forceinline__ void softmax(const kv_f32x16 (&s)[NS], float sl, vec (&w)[NS * NW]) {
+        float x = s[0][0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) x = fmaxf(x, s[i]);
-        const float m2 = fmaxf(m, kv_pair_max(x) * sl);
-        const float sub = m2 == -INFINITY ? 0.0f : m2;          // nothing seen yet: every weight is exp2(-inf)
-        const float keep = __builtin_amdgcn_exp2f(m - sub);
-        m = m2;
-        l *= keep;
+        for (int n = 0; n < NS; ++n)
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
+            for (int i = 0; i < 16; ++i) x = fmaxf(x, s[n][i]);
+        const float top = kv_pair_max(x) * sl;
+        if (__ballot(top > m + kSlack)) {
+            const float m2 = fmaxf(m, top);
+            const float keep = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - m2);
+            m = m2;
+            l *= keep;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[t][i] *= keep;
+            for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float e = __builtin_amdgcn_exp2f(s[i] * sl - sub);
-            l += e;
-            w[i / E][i % E] = (T)e;
+                for (int i = 0; i < 16; ++i) o[t][i] *= keep;
         }
+        const float sub = m == -INFINITY ? 0.0f : m;            // nothing seen yet: every weight is exp2(-inf)
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float e = __builtin_amdgcn_exp2f(s[n][i] * sl - sub);
+                l += e;
+                w[n * NW + i / E][i % E] = (T)e;
+            }
+    }
+    // A token whose values are not all finite, in a tile where some rows do not see it: zero took the place of its infinities and NaNs
+    // in the product (0 * inf is NaN), and the rows that do see it get them here.  value(c): the token's channel c.
+    template <typename V>
+    __device__ __forceinline__ void add_nonfinite(bool sees, V value) {
+        const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float x = value(dt * 32 + i / 4 * 8 + half * 4 + i % 4);
+                o[dt][i] += sees && !(fabsf(x) < INFINITY) ? x : 0.0f;
+                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // rare: few registers matter, not speed
+            }
     }
 };
+
+// 1 / l, or what makes a row that saw nothing 0; its lse.
+__device__ __forceinline__ float kv_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float kv_lse(float m, float l) { return l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f; }
