@@ -1,5 +1,10 @@
 // The blocks that each tile of queries will read (s3_block_select): scores of all candidates by matrix instructions, then the
 // top_b largest of each list by a radix search on the scores' ordered keys.
+//
+// Two forms.  sel_fused_kernel keeps a tile's keys in LDS: a workgroup takes some tiles of one sequence and head, all their rows in
+// registers, its wavefronts walk over different signatures, and a wavefront each then picks for a tile.  Where that would leave the
+// chip idle (few tiles, long contexts) or does not fit LDS, sel_score_kernel spreads the scores of a tile over many workgroups and leaves
+// the keys in scratch for sel_pick_kernel.
 #include "attn.h"
 
 namespace {
@@ -42,6 +47,195 @@ struct Tile {
     }
 };
 
+// 32 rows on their 8 bit grids as a matrix instruction's first operand: channel 16 s + 8 half + e of this lane's row at src (null: zeros).
+template <typename T, int D>
+__device__ __forceinline__ void grid_rows(const char* src, kv_bf16x8 (&a)[D / 16]) {
+    const int half = (threadIdx.x & 63) >> 5;
+    typename KvElem<T>::vec v[D / 16][8 / KvElem<T>::E];
+    typename KvElem<T>::vec zero = {};
+    unsigned big = 0;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+        for (int e = 0; e < 8 / KvElem<T>::E; ++e) {
+            v[s][e] = src ? *(const typename KvElem<T>::vec*)(src + half * (8 * (int)sizeof(T)) + s * 16 * (int)sizeof(T) + e * 16) : zero;
+            big = kv_magnitude(v[s][e], big);
+        }
+    big = max(big, (unsigned)__shfl_xor((int)big, 32));
+    bool ok;
+    const int ex = kv_grid_exp(big, ok);
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[s][e] = (__bf16)(ok ? kv_grid((float)v[s][e / KvElem<T>::E][e % KvElem<T>::E], ex) : 0.0f);
+}
+
+// The top largest of n keys, by one wavefront: key(i) for i < n, 0: no candidate; hist: 256 counters of this wavefront's own.
+// Four passes of eight bits find the threshold, a last one writes the blocks in ascending order and -1 behind them.
+template <typename K>
+__device__ __forceinline__ void pick_by_wave(K key, int n, int top, int* hist, int32_t* out) {
+    const int lane = threadIdx.x & 63;
+    unsigned thr = 0, mask = 0;
+    int left = top;                              // how many of the keys equal to the threshold are taken
+    for (int shift = 24; shift >= 0; shift -= 8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hist[lane * 4 + i] = 0;
+        s3_wave_fence();
+        for (int i = lane; i < n; i += 64) {
+            const unsigned k = key(i);
+            if ((k & mask) == thr && k) atomicAdd(&hist[k >> shift & 255u], 1);
+        }
+        s3_wave_fence();
+        int c[4], sum = 0;                       // this lane's bins, from the top: 255 - 4 lane ...
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += c[i] = hist[255 - 4 * lane - i];
+        s3_wave_fence();
+        const int incl = s3_wave_incl_scan(sum);
+        const uint64_t reach = __ballot(incl >= left);
+        int bin = 0, before = __builtin_amdgcn_readlane(incl, 63) - hist[0];      // fewer than asked for: the lowest bin
+        if (reach) {
+            const int l = __builtin_ctzll(reach);
+            before = __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(sum, l);
+            bin = 255 - 4 * l;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const int ci = __builtin_amdgcn_readlane(c[i], l);
+                if (before + ci < left && bin == 255 - 4 * l - i) {
+                    before += ci;
+                    --bin;
+                }
+            }
+        }
+        s3_wave_fence();
+        thr |= (unsigned)bin << shift;
+        left -= before;
+        mask |= 255u << shift;
+    }
+    int at = 0, eq = 0;
+    for (int base = 0; base < n; base += 64) {
+        const int i = base + lane;
+        const unsigned k = i < n ? key(i) : 0u;
+        const bool same = k == thr && k;
+        const uint64_t bs = __ballot(same), below = ((uint64_t)1 << lane) - 1;
+        const bool take = k > thr || (same && eq + __popcll(bs & below) < left);
+        const uint64_t bt = __ballot(take);
+        const int to = at + __popcll(bt & below);
+        if (take && to < top) out[to] = i;
+        at += __popcll(bt);
+        eq += __popcll(bs);
+    }
+    for (int i = at + lane; i < top; i += 64) out[i] = -1;
+}
+
+// tiles_wg tiles of one sequence and head.  Rows are dealt in fours, each four of one tile (a tile's last row repeated to fill them:
+// the largest score does not change), and lie in NSETS sets of 32 in registers; more than that are taken in further walks.
+template <typename T, int D, int NSETS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void sel_fused_kernel(SelectArgs p, int tiles_wg, int tiles) {
+    extern __shared__ unsigned lds_keys[];                       // [tiles_wg][nb] | [WAVES][256] counters
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = blockIdx.x % p.n_kv;
+    int* hist = (int*)(lds_keys + tiles_wg * p.nb) + wave * 256;
+    int s, j;
+    auto count = [&](int q) {
+        int f, m, l;
+        kv_seq(p.b, q, f, m, l);
+        return ((m + p.qb - 1) / p.qb + tiles_wg - 1) / tiles_wg;
+    };
+    const int group = blockIdx.x / p.n_kv;
+    const bool any = kv_find(p.b.n_seq, group, count, s, j);
+    // tiles of the sequences before, and of all
+    auto tiles_before = [&](int end) {
+        int sum = 0;
+        for (int base = 0; base < end; base += 64) {
+            const int q = base + lane;
+            int c = 0;
+            if (q < end) {
+                int f, m, l;
+                kv_seq(p.b, q, f, m, l);
+                c = (m + p.qb - 1) / p.qb;
+            }
+            sum += __builtin_amdgcn_readlane(s3_wave_incl_scan(c), 63);
+        }
+        return sum;
+    };
+    if (group == 0)                                              // lists past the last tile
+        for (int t = tiles_before(p.b.n_seq) + wave; t < tiles; t += WAVES)
+            for (int i = lane; i < p.top; i += 64) p.sel[((int64_t)t * p.n_kv + head) * p.top + i] = -1;
+    if (!any) return;
+    const int tile0 = tiles_before(s) + j * tiles_wg;            // the group's first tile
+    int first, n, len;
+    kv_seq(p.b, s, first, n, len);
+    const int t_first = j * tiles_wg, t_here = min(tiles_wg, (n + p.qb - 1) / p.qb - t_first);
+    const int end = min(n, (t_first + t_here) * p.qb);                                    // tokens of the group end here
+    const int last = len - n + end - 1;
+    const int nb = last < 0 ? 0 : min(min((last >> p.b.log_page) + 1, p.b.max_pages), p.nb);
+    for (int i = threadIdx.x; i < t_here * p.nb; i += WAVES * 64) lds_keys[i] = 0;
+    __syncthreads();
+    const int fours = (min(p.qb, n) * p.G + 3) / 4;                                        // of a tile
+    const bool whole_sets = fours % 8 == 0;
+    for (int f0 = 0; f0 < t_here * fours; f0 += NSETS * 8) {
+        kv_bf16x8 a[NSETS][D / 16];
+        int to[NSETS][4];                                        // where the scores of this lane's fours go, or -1
+#pragma unroll
+        for (int x = 0; x < NSETS; ++x) {
+            const int f = f0 + x * 8 + (col >> 2), t = f / fours;
+            const int tok0 = (t_first + t) * p.qb, rows = (min(n, tok0 + p.qb) - tok0) * p.G;
+            const char* src = nullptr;
+            if (t < t_here) {
+                const int r = tok0 * p.G + min((f - t * fours) * 4 + (col & 3), rows - 1), tk = r / p.G;
+                src = p.q + (int64_t)(first + tk) * p.q_ts + (int64_t)(head * p.G + r - tk * p.G) * p.q_hs;
+            }
+            grid_rows<T, D>(src, a[x]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int tq = (f0 + x * 8 + 2 * i + half) / fours;
+                to[x][i] = tq < t_here ? tq * p.nb : -1;
+            }
+        }
+        for (int b = wave * 32; b < nb; b += WAVES * 32) {
+            const int blk = b + col;
+            const int page = blk < nb ? kv_page(p.b, s, blk) : -1;
+            const __bf16* sg = p.sig + ((int64_t)max(page, 0) * p.n_kv + head) * D + half * 8;
+            kv_f32x16 c[NSETS];
+#pragma unroll
+            for (int x = 0; x < NSETS; ++x)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) c[x][i] = 0.0f;
+            kv_bf16x8 g[D / 16];
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) g[k] = *(const kv_bf16x8*)(sg + k * 16);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                for (int x = 0; x < NSETS; ++x) c[x] = kv_mma(a[x][k], g[k], c[x]);
+#pragma unroll
+            for (int x = 0; x < NSETS; ++x) {
+                float m[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m[i] = fmaxf(fmaxf(c[x][4 * i], c[x][4 * i + 1]), fmaxf(c[x][4 * i + 2], c[x][4 * i + 3]));
+                if (whole_sets) {
+                    const float best = kv_pair_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+                    if (half == 0 && page >= 0 && to[x][0] >= 0) atomicMax(&lds_keys[to[x][0] + blk], order_key(best));
+                } else if (page >= 0) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (to[x][i] >= 0) atomicMax(&lds_keys[to[x][i] + blk], order_key(m[i]));
+                }
+            }
+        }
+    }
+    __syncthreads();
+    for (int t = wave; t < t_here; t += WAVES) {
+        const int tok0 = (t_first + t) * p.qb, pos0 = max(0, len - n + tok0), pos1 = len - n + min(n, tok0 + p.qb) - 1;
+        const int own = p.tail > 0 ? (pos0 >> p.b.log_page) - p.tail + 1 : 1 << 30;         // blocks from here on are always taken
+        const int nt = pos1 < 0 ? 0 : min((pos1 >> p.b.log_page) + 1, nb);
+        const unsigned* keys = lds_keys + t * p.nb;
+        pick_by_wave([&](int i) { return keys[i] && (i < p.lead || i >= own) ? 0xffffffffu : keys[i]; }, nt, p.top, hist,
+                     p.sel + ((int64_t)(tile0 + t) * p.n_kv + head) * p.top);
+    }
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void sel_score_kernel(SelectArgs p) {
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wave = threadIdx.x >> 6;
@@ -55,39 +249,9 @@ __global__ __launch_bounds__(kThreads) void sel_score_kernel(SelectArgs p) {
     const int p0 = max(0, t.len - t.n + t.t0);
     const int own = p.tail > 0 ? (p0 >> p.b.log_page) - p.tail + 1 : 1 << 30;      // blocks from here on are always taken
     for (int r0 = t.t0 * p.G; r0 < t.t1 * p.G; r0 += 32) {
-        // 32 rows on their grids, as operand A: channel 16 s + 8 half + e of row col
         kv_bf16x8 a[D / 16];
-        const int r = r0 + col;
-        float x[D / 16][8];
-        unsigned big = 0;
-        if (r < t.t1 * p.G) {
-            const int tk = r / p.G, g = r - tk * p.G;
-            const char* src = p.q + (int64_t)(t.first + tk) * p.q_ts + (int64_t)(head * p.G + g) * p.q_hs + half * (8 * (int)sizeof(T));
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; e += KvElem<T>::E) {
-                    const auto v = *(const typename KvElem<T>::vec*)(src + (s * 16 + e) * (int)sizeof(T));
-#pragma unroll
-                    for (int i = 0; i < KvElem<T>::E; ++i) x[s][e + i] = (float)v[i];
-                }
-        } else {
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[s][e] = -INFINITY;        // a row that does not exist: zero, see below
-        }
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[s][e]) & 0x7fffffffu);
-        big = max(big, (unsigned)__shfl_xor((int)big, 32));
-        bool ok;
-        const int ex = kv_grid_exp(big, ok);
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a[s][e] = (__bf16)(ok ? kv_grid(x[s][e], ex) : 0.0f);
+        const int r = r0 + col, tk = r / p.G;
+        grid_rows<T, D>(r < t.t1 * p.G ? p.q + (int64_t)(t.first + tk) * p.q_ts + (int64_t)(head * p.G + r - tk * p.G) * p.q_hs : nullptr, a);
         const int rows = min(32, t.t1 * p.G - r0);
         for (int b = b0 + wave * 32; b < b1; b += kThreads / 2) {
             const int blk = b + col;
@@ -134,11 +298,11 @@ __global__ __launch_bounds__(kThreads) void sel_pick_kernel(SelectArgs p) {
             if ((k & mask) == thr && k) atomicAdd(&hist[k >> shift & 255u], 1);
         }
         __syncthreads();
-        if (tid == 0) {
-            int bin = 255;
-            for (; bin > 0 && hist[bin] < left; --bin) left -= hist[bin];
-            found[0] = (unsigned)bin;
-            found[1] = (unsigned)left;
+        int total;
+        const int c = hist[255 - tid], before = s3_block_excl_scan<kThreads>(c, wsum, total);      // this bin, and those above it
+        if ((before < left && left <= before + c) || (tid == 255 && total < left)) {
+            found[0] = (unsigned)(255 - tid);
+            found[1] = (unsigned)(left - before);
         }
         __syncthreads();
         thr |= found[0] << shift;
@@ -169,11 +333,63 @@ int select_blocks(const s3_kv_cache* c, const s3_kv_batch* b) {
     return (int)max((int64_t)1, min((int64_t)b->max_pages, ((int64_t)b->max_kv + c->page_size - 1) / c->page_size));
 }
 
+// How a call is shared out.
+struct SelectPlan {
+    bool fused;
+    int tiles_wg, sets, waves, nb;
+    int64_t tiles, groups;
+    SelectPlan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block) {
+        nb = select_blocks(c, b);
+        tiles = s3_block_tiles(b, q_block);
+        const int G = n_q / c->n_kv_heads, most = max(1, min(b->n_tokens, b->max_new));      // new tokens of a sequence
+        const int64_t fours = ((int64_t)min(q_block, most) * G + 3) / 4;
+        const int max_sets = c->d_head == 256 ? 2 : 4;
+        // as many tiles as fill the registers: every signature is read once per workgroup; not more than a sequence has, nor than
+        // 64 KB of keys (two workgroups a compute unit), and fewer where the chip would not be full
+        int64_t t = min(max(max_sets * 8 / fours, (int64_t)1), (int64_t)(most + q_block - 1) / q_block);
+        t = max((int64_t)1, min(t, (int64_t)16384 / nb));
+        while (t > 1 && tiles / t * c->n_kv_heads < 512) t /= 2;
+        tiles_wg = (int)t;
+        sets = t * fours <= 8 ? 1 : t * fours <= 16 || max_sets == 2 ? 2 : 4;
+        groups = (tiles + (int64_t)b->n_seq * (t - 1)) / t;
+        waves = sets == 1 && groups * c->n_kv_heads < 256 ? 16 : 4;
+        fused = nb <= 32768 && (nb <= 2048 || groups * c->n_kv_heads >= 64);
+    }
+    size_t workspace(int n_kv) const { return fused ? 0 : s3_align((size_t)tiles * n_kv * nb * 4); }
+};
+
+template <typename T, int D, int NSETS, int WAVES>
+int launch_fused(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
+    static S3LdsOnce once;
+    if (int rc = s3_allow_lds(once, (const void*)sel_fused_kernel<T, D, NSETS, WAVES>, 32768 * 4 + WAVES * 1024)) return rc;
+    hipLaunchKernelGGL((sel_fused_kernel<T, D, NSETS, WAVES>), dim3((unsigned)(plan.groups * p.n_kv)), dim3(WAVES * 64),
+                       plan.tiles_wg * plan.nb * 4 + WAVES * 1024, st, p, plan.tiles_wg, (int)plan.tiles);
+    S3_HIP(hipGetLastError());
+    return S3_OK;
+}
+template <typename T, int D>
+int launch_select(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
+    if (plan.fused) {
+        if (plan.waves == 16) return launch_fused<T, D, 1, 16>(p, plan, st);
+        if (plan.sets == 1) return launch_fused<T, D, 1, 4>(p, plan, st);
+        if (plan.sets == 2) return launch_fused<T, D, 2, 4>(p, plan, st);
+        if constexpr (D < 256) return launch_fused<T, D, 4, 4>(p, plan, st);
+    }
+    const dim3 grid((unsigned)(plan.tiles * p.n_kv), (unsigned)((p.nb + kScoreBlocks - 1) / kScoreBlocks));
+    if ((int64_t)grid.x * grid.y >= (int64_t)1 << 24 || grid.y > 65535) return s3_fail(S3_EINVAL, "s3_block_select: too many tiles in one call");
+    hipLaunchKernelGGL((sel_score_kernel<T, D>), grid, dim3(kThreads), 0, st, p);
+    S3_HIP(hipGetLastError());
+    hipLaunchKernelGGL(sel_pick_kernel, dim3(grid.x), dim3(kThreads), 0, st, p);
+    S3_HIP(hipGetLastError());
+    return S3_OK;
+}
+
 }  // namespace
 
 extern "C" size_t s3_block_select_workspace(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b) {
-    if (s3_kv_check("s3_block_select_workspace", c, b) || q_block < 1) return 0;
-    return s3_align((size_t)s3_block_tiles(b, q_block) * c->n_kv_heads * select_blocks(c, b) * 4);
+    (void)top_b;
+    if (s3_kv_check("s3_block_select_workspace", c, b) || q_block < 1 || n_q < 1 || n_q % c->n_kv_heads) return 0;
+    return SelectPlan(c, b, n_q, q_block).workspace(c->n_kv_heads);
 }
 
 extern "C" int s3_block_select(const s3_kv_cache* c, const s3_kv_batch* b, const void* q, int n_q, int64_t q_ts, int64_t q_hs, int q_block,
@@ -192,29 +408,16 @@ extern "C" int s3_block_select(const s3_kv_cache* c, const s3_kv_batch* b, const
     if (b->n_tokens)
         if (int rc = s3_kv_check_rows(fn, "q", c, q, q_ts, q_hs, n_q)) return rc;
     if (!sel) return s3_fail(S3_EINVAL, "%s: null sel", fn);
-    const size_t need = s3_block_select_workspace(c, b, n_q, q_block, top_b);
-    if (!ws || (uintptr_t)ws & 255) return s3_fail(S3_EINVAL, "%s: workspace is null or not 256-byte aligned", fn);
+    const SelectPlan plan(c, b, n_q, q_block);
+    const size_t need = plan.workspace(c->n_kv_heads);
+    if (need && (!ws || (uintptr_t)ws & 255)) return s3_fail(S3_EINVAL, "%s: workspace is null or not 256-byte aligned", fn);
     if (ws_bytes < need) return s3_fail(S3_ECAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
     if (tiles * c->n_kv_heads >= (int64_t)1 << 24) return s3_fail(S3_EINVAL, "%s: too many tiles in one call", fn);
-    const int es = c->dtype == S3_BF16 ? 2 : 4, nb = select_blocks(c, b);
+    const int es = c->dtype == S3_BF16 ? 2 : 4;
     SelectArgs p{s3_kv_batch_args(c, b), (const char*)q, q_ts * es, q_hs * es, (const __bf16*)c->sig, (unsigned*)ws, sel,
-                 c->n_kv_heads, n_q / c->n_kv_heads, q_block, top_b, lead, tail, nb};
+                 c->n_kv_heads, n_q / c->n_kv_heads, q_block, top_b, lead, tail, plan.nb};
     hipStream_t st = (hipStream_t)stream;
-    const dim3 grid((unsigned)(tiles * c->n_kv_heads), (unsigned)((nb + kScoreBlocks - 1) / kScoreBlocks));
-    if ((int64_t)grid.x * grid.y >= (int64_t)1 << 24 || grid.y > 65535) return s3_fail(S3_EINVAL, "%s: too many tiles in one call", fn);
-#define S3_SCORE(T, D) hipLaunchKernelGGL((sel_score_kernel<T, D>), grid, dim3(kThreads), 0, st, p)
-    if (c->dtype == S3_BF16) {
-        if (c->d_head == 64) S3_SCORE(__bf16, 64);
-        else if (c->d_head == 128) S3_SCORE(__bf16, 128);
-        else S3_SCORE(__bf16, 256);
-    } else {
-        if (c->d_head == 64) S3_SCORE(float, 64);
-        else if (c->d_head == 128) S3_SCORE(float, 128);
-        else S3_SCORE(float, 256);
-    }
-#undef S3_SCORE
-    S3_HIP(hipGetLastError());
-    hipLaunchKernelGGL(sel_pick_kernel, dim3(grid.x), dim3(kThreads), 0, st, p);
-    S3_HIP(hipGetLastError());
-    return S3_OK;
+    if (c->dtype == S3_BF16)
+        return c->d_head == 64 ? launch_select<__bf16, 64>(p, plan, st) : c->d_head == 128 ? launch_select<__bf16, 128>(p, plan, st) : launch_select<__bf16, 256>(p, plan, st);
+    return c->d_head == 64 ? launch_select<float, 64>(p, plan, st) : c->d_head == 128 ? launch_select<float, 128>(p, plan, st) : launch_select<float, 256>(p, plan, st);
 }

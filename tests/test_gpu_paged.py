@@ -290,6 +290,12 @@ def draw_sig(pr):
     ("bf16", 128, 16, 8, 2, [1, 1], [20000, 15000], 1, 64, 1, 1),      # more candidates than one pass of threads
     ("bf16", 128, 16, 4, 2, [10], [3], 4, 4, 1, 1),                   # tiles before the sequence
     ("bf16", 64, 16, 8, 2, [300], [400], 256, 40, 1, 1),               # many rows a tile
+    ("bf16", 128, 16, 28, 4, [100, 60], [900, 60], 1, 6, 1, 1),        # several tiles a workgroup, seven rows each
+    ("bf16", 128, 32, 32, 8, [200, 3, 0, 77], [900, 300, 40, 80], 8, 6, 1, 1),
+    ("fp32", 256, 16, 8, 4, [90], [2000], 4, 20, 1, 1),
+    ("bf16", 64, 16, 2, 2, [1], [50000], 1, 96, 1, 1),                 # few tiles, a long context: through scratch
+    ("fp32", 64, 16, 3, 1, [40], [40000], 16, 300, 1, 1),
+    ("bf16", 64, 16, 2, 1, [600], [700], 2, 5, 1, 1),
 ])
 def test_select(dtype, d, P, hq, hkv, new, kv, qb, top, lead, tail):
     pr = paged.Problem(11 + d + qb, dtype, d, P, hq, hkv, new, kv)
