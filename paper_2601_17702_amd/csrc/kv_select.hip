@@ -70,115 +70,163 @@ __device__ __forceinline__ void grid_rows(const char* src, kv_bf16x8 (&a)[D / 16
         for (int e = 0; e < 8; ++e) a[s][e] = (__bf16)(ok ? kv_grid((float)v[s][e / KvElem<T>::E][e % KvElem<T>::E], ex) : 0.0f);
 }
 
-// The top largest of n keys, by one wavefront: key(i) for i < n, 0: no candidate; hist: 256 counters of this wavefront's own.
-// Four passes of eight bits find the threshold, a last one writes the blocks in ascending order and -1 behind them.
-template <typename K>
-__device__ __forceinline__ void pick_by_wave(K key, int n, int top, int* hist, int32_t* out) {
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(s3_wave_incl_scan(x), 63); }
+
+// The top largest of keys[0 .. n - 1] (LDS, room for a multiple of 512; 0: no candidate; those below lead or from own on are always
+// taken), by one wavefront.  An interval of keys that holds the threshold is halved, a pass over LDS each time, until at most 64 keys
+// lie in it; those are ranked against each other, one a lane.  (Halving down to the threshold itself takes the key's bits in
+// rounds wherever two scores tie; a radix search's counters share their leading bits, and with them the counter: both took
+// three times as long.)  Ascending blocks, -1 behind them.  mid_keys: 64 words of this wavefront's own.
+__device__ __forceinline__ void pick_by_wave(unsigned* keys, int n, int lead, int own, int top, unsigned* mid_keys, int32_t* out) {
     const int lane = threadIdx.x & 63;
-    unsigned thr = 0, mask = 0;
-    int left = top;                              // how many of the keys equal to the threshold are taken
-    for (int shift = 24; shift >= 0; shift -= 8) {
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    auto read8 = [&](int base, unsigned (&k)[8]) {        // eight keys a lane at a time, whatever n is: their reads overlap
 #pragma unroll
-        for (int i = 0; i < 4; ++i) hist[lane * 4 + i] = 0;
-        s3_wave_fence();
-        for (int i = lane; i < n; i += 64) {
-            const unsigned k = key(i);
-            if ((k & mask) == thr && k) atomicAdd(&hist[k >> shift & 255u], 1);
+        for (int x = 0; x < 8; ++x) k[x] = keys[base + x * 64];
+    };
+    unsigned least = 0xffffffffu, most = 0;
+    int cand = 0, always = 0;
+    for (int base = lane; base < n + lane; base += 512) {
+        unsigned k[8];
+        read8(base, k);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int i = base + x * 64;
+            const bool in = k[x] && i < n, must = in && (i < lead || i >= own);
+            cand += in;
+            always += must;
+            least = min(least, in && !must ? k[x] : 0xffffffffu);
+            most = max(most, in && !must ? k[x] : 0u);
+            keys[i] = must ? 0xffffffffu : in ? k[x] : 0u;
         }
-        s3_wave_fence();
-        int c[4], sum = 0;                       // this lane's bins, from the top: 255 - 4 lane ...
+    }
+    s3_wave_fence();
+    cand = wave_sum(cand);
+    always = wave_sum(always);
+    unsigned thr = 1;                            // taken: keys above thr, and the first `equal` of those at it
+    int equal = n;
+    if (cand > top) {
+        if (always >= top) {
+            thr = 0xffffffffu;
+            equal = top;
+        } else {
+            unsigned lo = ~s3_wave_max_u32(~least), hi = s3_wave_max_u32(most) + 1;      // more than `top` from lo on, at most that from hi on
+            int from_lo = cand, from_hi = always;
+            while (hi - lo > 1 && from_lo - from_hi > 64) {
+                const unsigned mid = lo + (hi - lo) / 2;
+                int c = 0;
+                for (int base = 0; base < n; base += 512) {
+                    unsigned k[8];
+                    read8(base + lane, k);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += c[i] = hist[255 - 4 * lane - i];
-        s3_wave_fence();
-        const int incl = s3_wave_incl_scan(sum);
-        const uint64_t reach = __ballot(incl >= left);
-        int bin = 0, before = __builtin_amdgcn_readlane(incl, 63) - hist[0];      // fewer than asked for: the lowest bin
-        if (reach) {
-            const int l = __builtin_ctzll(reach);
-            before = __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(sum, l);
-            bin = 255 - 4 * l;
+                    for (int x = 0; x < 8; ++x) c += __popcll(__ballot(k[x] >= mid));
+                }
+                if (c > top) {
+                    lo = mid;
+                    from_lo = c;
+                } else {
+                    hi = mid;
+                    from_hi = c;
+                }
+            }
+            const int need = top - from_hi;              // of those in the interval
+            thr = lo;
+            equal = need;
+            if (from_lo - from_hi <= 64) {
+                int m = 0;
+                for (int base = 0; base < n; base += 512) {
+                    unsigned k[8];
+                    read8(base + lane, k);
 #pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                const int ci = __builtin_amdgcn_readlane(c[i], l);
-                if (before + ci < left && bin == 255 - 4 * l - i) {
-                    before += ci;
-                    --bin;
+                    for (int x = 0; x < 8; ++x) {
+                        const bool in = k[x] >= lo && k[x] < hi;
+                        const uint64_t b = __ballot(in);
+                        if (in) mid_keys[m + __popcll(b & below)] = k[x];
+                        m += __popcll(b);
+                    }
+                }
+                s3_wave_fence();
+                const unsigned mine = lane < m ? mid_keys[lane] : 0u;
+                int rank = 0, greater = 0;               // keys before this one: greater, or equal and of a lower block
+                for (int i = 0; i < m; ++i) {
+                    const unsigned k = (unsigned)__builtin_amdgcn_readlane((int)mine, i);
+                    greater += k > mine;
+                    rank += k > mine || (k == mine && i < lane);
+                }
+                if (need > 0) {
+                    const int l = __builtin_ctzll(__ballot(lane < m && rank == need - 1));
+                    thr = (unsigned)__builtin_amdgcn_readlane((int)mine, l);
+                    equal = need - __builtin_amdgcn_readlane(greater, l);
+                } else {                                 // nothing of it
+                    thr = hi - 1;
+                    equal = 0;
                 }
             }
         }
-        s3_wave_fence();
-        thr |= (unsigned)bin << shift;
-        left -= before;
-        mask |= 255u << shift;
     }
     int at = 0, eq = 0;
-    for (int base = 0; base < n; base += 64) {
-        const int i = base + lane;
-        const unsigned k = i < n ? key(i) : 0u;
-        const bool same = k == thr && k;
-        const uint64_t bs = __ballot(same), below = ((uint64_t)1 << lane) - 1;
-        const bool take = k > thr || (same && eq + __popcll(bs & below) < left);
-        const uint64_t bt = __ballot(take);
-        const int to = at + __popcll(bt & below);
-        if (take && to < top) out[to] = i;
-        at += __popcll(bt);
-        eq += __popcll(bs);
+    for (int base = lane; base < n + lane; base += 512) {
+        unsigned k[8];
+        read8(base, k);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const uint64_t bs = __ballot(k[x] == thr);
+            const bool take = k[x] > thr || (k[x] == thr && eq + __popcll(bs & below) < equal);
+            const uint64_t bt = __ballot(take);
+            const int to = at + __popcll(bt & below);
+            if (take && to < top) out[to] = base + x * 64;
+            at += __popcll(bt);
+            eq += __popcll(bs);
+        }
     }
     for (int i = at + lane; i < top; i += 64) out[i] = -1;
 }
 
 // tiles_wg tiles of one sequence and head.  Rows are dealt in fours, each four of one tile (a tile's last row repeated to fill them:
 // the largest score does not change), and lie in NSETS sets of 32 in registers; more than that are taken in further walks.
-template <typename T, int D, int NSETS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void sel_fused_kernel(SelectArgs p, int tiles_wg, int tiles) {
-    extern __shared__ unsigned lds_keys[];                       // [tiles_wg][nb] | [WAVES][256] counters
+// WHOLE: a tile is whole sets.
+template <typename T, int D, int NSETS, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(WAVES * 64, D == 256 || WAVES == 4 ? 2 : 4) void sel_fused_kernel(SelectArgs p, int tiles_wg, int tiles) {
+    extern __shared__ unsigned lds_keys[];                       // [tiles_wg][stride] | [WAVES][64] | rows (NSETS > 1)
+    const int stride = (p.nb + 511) & ~511;
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % p.n_kv;
-    int* hist = (int*)(lds_keys + tiles_wg * p.nb) + wave * 256;
-    int s, j;
-    auto count = [&](int q) {
-        int f, m, l;
-        kv_seq(p.b, q, f, m, l);
-        return ((m + p.qb - 1) / p.qb + tiles_wg - 1) / tiles_wg;
-    };
     const int group = blockIdx.x / p.n_kv;
-    const bool any = kv_find(p.b.n_seq, group, count, s, j);
-    // tiles of the sequences before, and of all
-    auto tiles_before = [&](int end) {
-        int sum = 0;
-        for (int base = 0; base < end; base += 64) {
-            const int q = base + lane;
-            int c = 0;
-            if (q < end) {
-                int f, m, l;
-                kv_seq(p.b, q, f, m, l);
-                c = (m + p.qb - 1) / p.qb;
-            }
-            sum += __builtin_amdgcn_readlane(s3_wave_incl_scan(c), 63);
+    // the group's sequence, and the tiles before it and of all: every workgroup reads the sequences' lengths once
+    int s = -1, j = 0, first = 0, n = 0, len = 0, tile0 = 0, tiles_all = 0, groups = 0;
+    for (int base = 0; base < p.b.n_seq && (s < 0 || group == 0); base += 64) {
+        int f = 0, m = 0, l = 0;
+        if (base + lane < p.b.n_seq) kv_seq(p.b, base + lane, f, m, l);
+        const int c = (m + p.qb - 1) / p.qb, g = (c + tiles_wg - 1) / tiles_wg;
+        const int ci = s3_wave_incl_scan(c), gi = s3_wave_incl_scan(g);
+        const int g_sum = __builtin_amdgcn_readlane(gi, 63);
+        if (s < 0 && group < groups + g_sum) {
+            const int x = __builtin_ctzll(__ballot(groups + gi > group));
+            s = base + x;
+            j = group - groups - (__builtin_amdgcn_readlane(gi, x) - __builtin_amdgcn_readlane(g, x));
+            first = __builtin_amdgcn_readlane(f, x);
+            n = __builtin_amdgcn_readlane(m, x);
+            len = __builtin_amdgcn_readlane(l, x);
+            tile0 = tiles_all + __builtin_amdgcn_readlane(ci, x) - __builtin_amdgcn_readlane(c, x) + j * tiles_wg;
         }
-        return sum;
-    };
+        tiles_all += __builtin_amdgcn_readlane(ci, 63);
+        groups += g_sum;
+    }
     if (group == 0)                                              // lists past the last tile
-        for (int t = tiles_before(p.b.n_seq) + wave; t < tiles; t += WAVES)
+        for (int t = tiles_all + wave; t < tiles; t += WAVES)
             for (int i = lane; i < p.top; i += 64) p.sel[((int64_t)t * p.n_kv + head) * p.top + i] = -1;
-    if (!any) return;
-    const int tile0 = tiles_before(s) + j * tiles_wg;            // the group's first tile
-    int first, n, len;
-    kv_seq(p.b, s, first, n, len);
+    if (s < 0) return;
     const int t_first = j * tiles_wg, t_here = min(tiles_wg, (n + p.qb - 1) / p.qb - t_first);
     const int end = min(n, (t_first + t_here) * p.qb);                                    // tokens of the group end here
     const int last = len - n + end - 1;
     const int nb = last < 0 ? 0 : min(min((last >> p.b.log_page) + 1, p.b.max_pages), p.nb);
-    for (int i = threadIdx.x; i < t_here * p.nb; i += WAVES * 64) lds_keys[i] = 0;
+    for (int i = threadIdx.x; i < t_here * stride; i += WAVES * 64) lds_keys[i] = 0;
     __syncthreads();
-    const int fours = (min(p.qb, n) * p.G + 3) / 4;                                        // of a tile
-    const bool whole_sets = fours % 8 == 0;
+    const int fours = WHOLE ? p.qb * p.G / 4 : (min(p.qb, n) * p.G + 3) / 4;               // of a tile
     for (int f0 = 0; f0 < t_here * fours; f0 += NSETS * 8) {
         kv_bf16x8 a[NSETS][D / 16];
-        int to[NSETS][4];                                        // where the scores of this lane's fours go, or -1
-#pragma unroll
-        for (int x = 0; x < NSETS; ++x) {
+        auto rows_of = [&](int x) {
             const int f = f0 + x * 8 + (col >> 2), t = f / fours;
             const int tok0 = (t_first + t) * p.qb, rows = (min(n, tok0 + p.qb) - tok0) * p.G;
             const char* src = nullptr;
@@ -187,34 +235,67 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void sel_fused_ker
                 src = p.q + (int64_t)(first + tk) * p.q_ts + (int64_t)(head * p.G + r - tk * p.G) * p.q_hs;
             }
             grid_rows<T, D>(src, a[x]);
+        };
+        int to[NSETS][WHOLE ? 1 : 4];                            // where the scores of this lane's fours go, or -1
+        if constexpr (NSETS == 1) {
+            rows_of(0);
+        } else {
+            // a set is put on its grid by one wavefront and handed to the others
+            kv_bf16x8* rows = (kv_bf16x8*)(lds_keys + tiles_wg * stride + WAVES * 64);
+            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int tq = (f0 + x * 8 + 2 * i + half) / fours;
-                to[x][i] = tq < t_here ? tq * p.nb : -1;
+            for (int x = 0; x < NSETS; ++x)
+                if (x % WAVES == wave) {
+                    rows_of(x);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) rows[(x * (D / 16) + k) * 64 + lane] = a[x][k];
+                }
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < NSETS; ++x)
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) a[x][k] = rows[(x * (D / 16) + k) * 64 + lane];
+        }
+#pragma unroll
+        for (int x = 0; x < NSETS; ++x) {
+#pragma unroll
+            for (int i = 0; i < (WHOLE ? 1 : 4); ++i) {
+                const int tq = (f0 + x * 8 + (WHOLE ? 0 : 2 * i + half)) / fours;
+                to[x][i] = tq < t_here ? tq * stride : -1;
             }
         }
+        // the next signatures are on their way from the moment that this walk step's are used up
+        constexpr int K = D / 16;
+        auto lookup = [&](int blk) { return blk < nb ? kv_page(p.b, s, blk) : -1; };
+        auto sig_of = [&](int page) { return p.sig + ((int64_t)max(page, 0) * p.n_kv + head) * D + half * 8; };
+        kv_bf16x8 g[K];
+        int page = lookup(wave * 32 + col), next = lookup((wave + WAVES) * 32 + col);
+#pragma unroll
+        for (int k = 0; k < K; ++k) g[k] = *(const kv_bf16x8*)(sig_of(page) + k * 16);
         for (int b = wave * 32; b < nb; b += WAVES * 32) {
             const int blk = b + col;
-            const int page = blk < nb ? kv_page(p.b, s, blk) : -1;
-            const __bf16* sg = p.sig + ((int64_t)max(page, 0) * p.n_kv + head) * D + half * 8;
+            const __bf16* sg = sig_of(next);
+            const int after = lookup(blk + 2 * WAVES * 32);
             kv_f32x16 c[NSETS];
 #pragma unroll
             for (int x = 0; x < NSETS; ++x)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) c[x][i] = 0.0f;
-            kv_bf16x8 g[D / 16];
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) g[k] = *(const kv_bf16x8*)(sg + k * 16);
+            for (int y = 0; y < 2; ++y) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
+                for (int k = y * K / 2; k < (y + 1) * K / 2; ++k)
 #pragma unroll
-                for (int x = 0; x < NSETS; ++x) c[x] = kv_mma(a[x][k], g[k], c[x]);
+                    for (int x = 0; x < NSETS; ++x) c[x] = kv_mma(a[x][k], g[k], c[x]);
+#pragma unroll
+                for (int k = y * K / 2; k < (y + 1) * K / 2; ++k) g[k] = *(const kv_bf16x8*)(sg + k * 16);
+            }
 #pragma unroll
             for (int x = 0; x < NSETS; ++x) {
                 float m[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) m[i] = fmaxf(fmaxf(c[x][4 * i], c[x][4 * i + 1]), fmaxf(c[x][4 * i + 2], c[x][4 * i + 3]));
-                if (whole_sets) {
+                if constexpr (WHOLE) {
                     const float best = kv_pair_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
                     if (half == 0 && page >= 0 && to[x][0] >= 0) atomicMax(&lds_keys[to[x][0] + blk], order_key(best));
                 } else if (page >= 0) {
@@ -223,6 +304,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void sel_fused_ker
                         if (to[x][i] >= 0) atomicMax(&lds_keys[to[x][i] + blk], order_key(m[i]));
                 }
             }
+            page = next;
+            next = after;
         }
     }
     __syncthreads();
@@ -230,8 +313,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void sel_fused_ker
         const int tok0 = (t_first + t) * p.qb, pos0 = max(0, len - n + tok0), pos1 = len - n + min(n, tok0 + p.qb) - 1;
         const int own = p.tail > 0 ? (pos0 >> p.b.log_page) - p.tail + 1 : 1 << 30;         // blocks from here on are always taken
         const int nt = pos1 < 0 ? 0 : min((pos1 >> p.b.log_page) + 1, nb);
-        const unsigned* keys = lds_keys + t * p.nb;
-        pick_by_wave([&](int i) { return keys[i] && (i < p.lead || i >= own) ? 0xffffffffu : keys[i]; }, nt, p.top, hist,
+        pick_by_wave(lds_keys + t * stride, nt, p.lead, own, p.top, lds_keys + tiles_wg * stride + wave * 64,
                      p.sel + ((int64_t)(tile0 + t) * p.n_kv + head) * p.top);
     }
 }
@@ -335,7 +417,7 @@ int select_blocks(const s3_kv_cache* c, const s3_kv_batch* b) {
 
 // How a call is shared out.
 struct SelectPlan {
-    bool fused;
+    bool fused, whole;
     int tiles_wg, sets, waves, nb;
     int64_t tiles, groups;
     SelectPlan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block) {
@@ -345,35 +427,39 @@ struct SelectPlan {
         const int64_t fours = ((int64_t)min(q_block, most) * G + 3) / 4;
         const int max_sets = c->d_head == 256 ? 2 : 4;
         // as many tiles as fill the registers: every signature is read once per workgroup; not more than a sequence has, nor than
-        // 64 KB of keys (two workgroups a compute unit), and fewer where the chip would not be full
+        // 48 KB of keys (two workgroups a compute unit), and fewer where the chip would not be full
         int64_t t = min(max(max_sets * 8 / fours, (int64_t)1), (int64_t)(most + q_block - 1) / q_block);
-        t = max((int64_t)1, min(t, (int64_t)16384 / nb));
+        t = max((int64_t)1, min(t, (int64_t)12288 / ((nb + 511) & ~511)));
         while (t > 1 && tiles / t * c->n_kv_heads < 512) t /= 2;
         tiles_wg = (int)t;
         sets = t * fours <= 8 ? 1 : t * fours <= 16 || max_sets == 2 ? 2 : 4;
         groups = (tiles + (int64_t)b->n_seq * (t - 1)) / t;
-        waves = sets == 1 && groups * c->n_kv_heads < 256 ? 16 : 4;
-        fused = nb <= 32768 && (nb <= 2048 || groups * c->n_kv_heads >= 64);
+        whole = q_block <= most && (int64_t)q_block * G % 32 == 0;
+        waves = sets == 1 && groups * c->n_kv_heads < 256 ? 16 : 8;
+        fused = nb <= 30720 && (nb <= 2048 || groups * c->n_kv_heads >= 64);
     }
     size_t workspace(int n_kv) const { return fused ? 0 : s3_align((size_t)tiles * n_kv * nb * 4); }
 };
 
-template <typename T, int D, int NSETS, int WAVES>
+template <typename T, int D, int NSETS, int WAVES, bool WHOLE>
 int launch_fused(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
+    constexpr int extra = WAVES * 256 + (NSETS > 1 ? NSETS * 32 * D * 2 : 0);
     static S3LdsOnce once;
-    if (int rc = s3_allow_lds(once, (const void*)sel_fused_kernel<T, D, NSETS, WAVES>, 32768 * 4 + WAVES * 1024)) return rc;
-    hipLaunchKernelGGL((sel_fused_kernel<T, D, NSETS, WAVES>), dim3((unsigned)(plan.groups * p.n_kv)), dim3(WAVES * 64),
-                       plan.tiles_wg * plan.nb * 4 + WAVES * 1024, st, p, plan.tiles_wg, (int)plan.tiles);
+    if (int rc = s3_allow_lds(once, (const void*)sel_fused_kernel<T, D, NSETS, WAVES, WHOLE>, 30720 * 4 + extra)) return rc;
+    hipLaunchKernelGGL((sel_fused_kernel<T, D, NSETS, WAVES, WHOLE>), dim3((unsigned)(plan.groups * p.n_kv)), dim3(WAVES * 64),
+                       plan.tiles_wg * ((plan.nb + 511) & ~511) * 4 + extra, st, p, plan.tiles_wg, (int)plan.tiles);
     S3_HIP(hipGetLastError());
     return S3_OK;
 }
 template <typename T, int D>
 int launch_select(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
     if (plan.fused) {
-        if (plan.waves == 16) return launch_fused<T, D, 1, 16>(p, plan, st);
-        if (plan.sets == 1) return launch_fused<T, D, 1, 4>(p, plan, st);
-        if (plan.sets == 2) return launch_fused<T, D, 2, 4>(p, plan, st);
-        if constexpr (D < 256) return launch_fused<T, D, 4, 4>(p, plan, st);
+        if constexpr (D < 256) {
+            if (plan.waves == 16) return launch_fused<T, D, 1, 16, false>(p, plan, st);
+            if (plan.sets == 4) return plan.whole ? launch_fused<T, D, 4, 4, true>(p, plan, st) : launch_fused<T, D, 4, 4, false>(p, plan, st);
+        }
+        if (plan.sets == 1) return launch_fused<T, D, 1, 8, false>(p, plan, st);
+        return plan.whole ? launch_fused<T, D, 2, 4, true>(p, plan, st) : launch_fused<T, D, 2, 4, false>(p, plan, st);
     }
     const dim3 grid((unsigned)(plan.tiles * p.n_kv), (unsigned)((p.nb + kScoreBlocks - 1) / kScoreBlocks));
     if ((int64_t)grid.x * grid.y >= (int64_t)1 << 24 || grid.y > 65535) return s3_fail(S3_EINVAL, "s3_block_select: too many tiles in one call");
