@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libs3attn.so")
@@ -23,14 +24,9 @@ class S3Error(RuntimeError):
         self.code = code
 
 
-class _KVCacheStruct(C.Structure):
-    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("sig", C.c_void_p), ("dtype", C.c_int), ("n_pages", C.c_int),
-                ("page_size", C.c_int), ("n_kv_heads", C.c_int), ("d_head", C.c_int)]
-
-
-class _KVBatchStruct(C.Structure):
-    _fields_ = [("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("block_table", C.c_void_p), ("table_stride", C.c_int64),
-                ("n_seq", C.c_int), ("n_tokens", C.c_int), ("max_pages", C.c_int), ("max_new", C.c_int), ("max_kv", C.c_int)]
+# s3_kv_cache and s3_kv_batch of the header, packed into bytes (a call takes their address; a ctypes structure takes four times
+# as long to fill)
+_KV_CACHE, _KV_BATCH = struct.Struct("PPPiiiii4x"), struct.Struct("PPPqiiiii4x")
 
 
 def lib():
@@ -100,24 +96,23 @@ def lib():
         cf = C.c_float
         L.s3_sae_train_step.argtypes = [vp, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, cf, cf, cf, cf, ci, vp, vp, vp, vp, sz, vp]
         L.s3_sae_train_step.restype = ci
-        cache_p, batch_p = C.POINTER(_KVCacheStruct), C.POINTER(_KVBatchStruct)
         L.s3_rope_table.argtypes = [vp, i64, ci, C.c_double, vp]
         L.s3_rope_table.restype = ci
-        L.s3_kv_append.argtypes = [cache_p, batch_p, vp, i64, i64, vp, i64, i64, vp, i64, ci, ci, vp, vp, ci, i64, i64, vp, vp]
+        L.s3_kv_append.argtypes = [vp, vp, vp, i64, i64, vp, i64, i64, vp, i64, ci, ci, vp, vp, ci, i64, i64, vp, vp]
         L.s3_kv_append.restype = ci
-        L.s3_paged_attention_workspace.argtypes = [cache_p, batch_p, ci]
+        L.s3_paged_attention_workspace.argtypes = [vp, vp, ci]
         L.s3_paged_attention_workspace.restype = sz
-        L.s3_paged_attention.argtypes = [cache_p, batch_p, vp, ci, i64, i64, cf, ci, vp, vp, vp, sz, vp]
+        L.s3_paged_attention.argtypes = [vp, vp, vp, ci, i64, i64, cf, ci, vp, vp, vp, sz, vp]
         L.s3_paged_attention.restype = ci
-        L.s3_block_tiles.argtypes = [batch_p, ci]
+        L.s3_block_tiles.argtypes = [vp, ci]
         L.s3_block_tiles.restype = i64
-        L.s3_block_select_workspace.argtypes = [cache_p, batch_p, ci, ci, ci]
+        L.s3_block_select_workspace.argtypes = [vp, vp, ci, ci, ci]
         L.s3_block_select_workspace.restype = sz
-        L.s3_block_select.argtypes = [cache_p, batch_p, vp, ci, i64, i64, ci, ci, ci, ci, vp, vp, sz, vp]
+        L.s3_block_select.argtypes = [vp, vp, vp, ci, i64, i64, ci, ci, ci, ci, vp, vp, sz, vp]
         L.s3_block_select.restype = ci
-        L.s3_block_attention_workspace.argtypes = [cache_p, batch_p, ci, ci, ci]
+        L.s3_block_attention_workspace.argtypes = [vp, vp, ci, ci, ci]
         L.s3_block_attention_workspace.restype = sz
-        L.s3_block_attention.argtypes = [cache_p, batch_p, vp, ci, i64, i64, vp, ci, ci, cf, vp, vp, vp, sz, vp]
+        L.s3_block_attention.argtypes = [vp, vp, vp, ci, i64, i64, vp, ci, ci, cf, vp, vp, vp, sz, vp]
         L.s3_block_attention.restype = ci
         for name in ("s3_sae_encode_topk", "s3_sae_encode_topk_stream", "s3_index_create", "s3_index_append", "s3_index_finalize",
                      "s3_index_csr", "s3_index_build", "s3_coactivate_score"):
@@ -464,6 +459,18 @@ class SaeTrainer:
         return self.loss, ids, grads
 
 
+def _torch():
+    """torch, imported on the first use of the cache and not with the package."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
+_torch_module = None
+
+
 def rope_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device="cuda"):
     """s3_rope_table: cos | sin of positions 0 .. n_pos - 1, [n_pos, rot_dim] fp32."""
     import torch
@@ -499,104 +506,122 @@ class KVCache:
             return t
         self.k, self.v = array("k", k, dtype), array("v", v, dtype)
         self.sig = array("sig", sig, torch.bfloat16) if signatures or sig is not None else None
+        lib()
+        self.scale = d_head ** -0.5
         self.dtype, self.page_size, self.n_kv_heads, self.d_head, self.n_pages = dtype, page_size, n_kv_heads, d_head, n_pages
-        self._c = _KVCacheStruct(_ptr(self.k), _ptr(self.v), _ptr(self.sig), _dtype_code(self.k), n_pages, page_size, n_kv_heads, d_head)
+        self._c = _KV_CACHE.pack(_ptr(self.k), _ptr(self.v), _ptr(self.sig) or 0, _dtype_code(self.k), n_pages, page_size, n_kv_heads, d_head)
 
+    # These run before every launch: as few attribute reads as the checks allow.
     def _batch(self, n_tokens, kv_len, block_table, q_start, max_new, max_kv):
-        import torch
-        i32 = torch.int32
-        assert kv_len.is_cuda and kv_len.dtype == i32 and kv_len.dim() == 1 and kv_len.is_contiguous()
-        n_seq = kv_len.shape[0]
-        assert block_table.is_cuda and block_table.dtype == i32 and block_table.dim() == 2 and block_table.shape[0] == n_seq
-        assert block_table.shape[1] == 0 or block_table.stride(1) == 1
-        width = block_table.shape[1]
+        i32 = kv_len.dtype
+        n_seq, = kv_len.shape
+        rows, width = block_table.shape
+        stride, inner = block_table.stride()
+        assert i32 is _torch().int32 and block_table.dtype is i32 and kv_len.is_cuda and block_table.is_cuda
+        assert rows == n_seq and (inner == 1 or width <= 1) and kv_len.is_contiguous()
+        qs = 0
         if q_start is not None:
-            assert q_start.is_cuda and q_start.dtype == i32 and q_start.shape == (n_seq + 1,) and q_start.is_contiguous()
+            assert q_start.dtype is i32 and q_start.is_cuda and q_start.shape == (n_seq + 1,) and q_start.is_contiguous()
+            qs = q_start.data_ptr()
         else:
             assert n_tokens == n_seq
             max_new = 1
-        return _KVBatchStruct(_ptr(q_start), kv_len.data_ptr(), block_table.data_ptr(), max(block_table.stride(0), width), n_seq, n_tokens,
-                              width, n_tokens if max_new is None else max_new, width * self.page_size if max_kv is None else max_kv)
+        return _KV_BATCH.pack(qs, kv_len.data_ptr(), block_table.data_ptr(), stride if rows > 1 and stride > width else width, n_seq, n_tokens, width,
+                              n_tokens if max_new is None else max_new, width * self.page_size if max_kv is None else max_kv)
 
     def _rows(self, x, heads=None):
-        assert x.is_cuda and x.dim() == 3 and x.dtype == self.dtype and x.shape[2] == self.d_head and x.stride(2) == 1
-        assert heads is None or x.shape[1] == heads
-        return x.data_ptr(), x.stride(0), x.stride(1)
+        _, n, d = x.shape
+        ts, hs, inner = x.stride()
+        assert x.dtype is self.dtype and x.is_cuda and d == self.d_head and inner == 1 and (heads is None or n == heads)
+        return x.data_ptr(), ts, hs
 
     def append(self, k, v, kv_len, block_table, q_start=None, rope=None, interleaved: bool = False, positions=None, q=None, q_out=None,
                max_new=None):
         """s3_kv_append: k, v [n_tokens, n_kv_heads, d_head] into their pages, keys (and q) rotated by rope (rope_table) first.
         Returns the rotated q, or None without q."""
-        import torch
         T = k.shape[0]
+        kp, kt, kh = self._rows(k, self.n_kv_heads)
+        vp, vt, vh = self._rows(v, self.n_kv_heads)
         assert v.shape[0] == T
         b = self._batch(T, kv_len, block_table, q_start, max_new, None)
+        rp = n_pos = rot = n_q = qp = qt = qh = op = 0
         if rope is not None:
-            assert rope.is_cuda and rope.is_contiguous() and rope.dtype == torch.float32 and rope.dim() == 2
+            n_pos, rot = rope.shape
+            assert rope.is_cuda and rope.is_contiguous() and rope.dtype is _torch().float32
+            rp = rope.data_ptr()
         if positions is not None:
-            assert positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32 and positions.numel() == T
-        qa, n_q = (None, 0, 0), 0
+            assert positions.is_cuda and positions.is_contiguous() and positions.dtype is kv_len.dtype and positions.shape == (T,)
         if q is not None:
-            qa, n_q = self._rows(q), q.shape[1]
+            qp, qt, qh = self._rows(q)
+            n_q = q.shape[1]
             assert q.shape[0] == T
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            assert q_out.is_contiguous() and q_out.shape == q.shape and q_out.dtype == q.dtype
-        _check(lib().s3_kv_append(self._c, b, *self._rows(k, self.n_kv_heads), *self._rows(v, self.n_kv_heads), _ptr(rope),
-                                  0 if rope is None else rope.shape[0], 0 if rope is None else rope.shape[1], int(interleaved),
-                                  _ptr(positions), qa[0], n_q, qa[1], qa[2], _ptr(q_out), _stream()))
+                q_out = _torch().empty_like(q, memory_format=_torch().contiguous_format)
+            assert q_out.shape == q.shape and q_out.dtype is q.dtype and q_out.is_contiguous() and q_out.is_cuda
+            op = q_out.data_ptr()
+        rc = _lib.s3_kv_append(self._c, b, kp, kt, kh, vp, vt, vh, rp, n_pos, rot, interleaved, _ptr(positions), qp, n_q, qt, qh, op, _stream())
+        if rc:
+            _check(rc)
         return q_out
 
     def _out(self, q, out, want_lse, need, ws):
-        import torch
+        torch = _torch()
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        else:
+            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.is_cuda
+        lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
         if ws is None and need:
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            ws = q.new_empty(need, dtype=torch.uint8)
         return out, lse, ws
 
     def attention(self, q, kv_len, block_table, q_start=None, scale=None, window: int = 0, max_new=None, max_kv=None, out=None,
                   want_lse: bool = False, ws=None):
         """s3_paged_attention: q [n_tokens, n_q_heads, d_head] over all that the sequences hold (append first).  Returns
         (out, lse fp32 [n_tokens, n_q_heads] | None)."""
-        b = self._batch(q.shape[0], kv_len, block_table, q_start, max_new, max_kv)
-        qa, n_q = self._rows(q), q.shape[1]
-        need = int(lib().s3_paged_attention_workspace(self._c, b, n_q))
+        T, n_q, _ = q.shape
+        b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
+        qp, qt, qh = self._rows(q)
+        need = _lib.s3_paged_attention_workspace(self._c, b, n_q)
         out, lse, ws = self._out(q, out, want_lse, need, ws)
-        _check(lib().s3_paged_attention(self._c, b, qa[0], n_q, qa[1], qa[2], self.d_head ** -0.5 if scale is None else scale, window,
-                                        _ptr(out), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+        rc = _lib.s3_paged_attention(self._c, b, qp, n_q, qt, qh, self.scale if scale is None else scale, window, out.data_ptr(),
+                                     _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+        if rc:
+            _check(rc)
         return out, lse
 
     def select(self, q, kv_len, block_table, top_b: int, q_start=None, q_block: int = 1, lead: int = 1, tail: int = 1, max_new=None,
                max_kv=None, ws=None):
         """s3_block_select: per tile of q_block queries and key/value head the top_b blocks (pages) whose signatures score
         highest, the first `lead` and the last `tail` among them.  Returns sel int32 [tiles, n_kv_heads, top_b], ascending, -1 filled."""
-        import torch
-        b = self._batch(q.shape[0], kv_len, block_table, q_start, max_new, max_kv)
-        qa, n_q = self._rows(q), q.shape[1]
-        tiles = int(lib().s3_block_tiles(b, q_block))
-        sel = torch.empty((tiles, self.n_kv_heads, top_b), dtype=torch.int32, device=q.device)
-        need = int(lib().s3_block_select_workspace(self._c, b, n_q, q_block, top_b))
+        torch = _torch()
+        T, n_q, _ = q.shape
+        b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
+        qp, qt, qh = self._rows(q)
+        sel = q.new_empty((_lib.s3_block_tiles(b, q_block), self.n_kv_heads, top_b), dtype=torch.int32)
+        need = _lib.s3_block_select_workspace(self._c, b, n_q, q_block, top_b)
         if ws is None and need:
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _check(lib().s3_block_select(self._c, b, qa[0], n_q, qa[1], qa[2], q_block, top_b, lead, tail, _ptr(sel),
-                                     _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+            ws = q.new_empty(need, dtype=torch.uint8)
+        rc = _lib.s3_block_select(self._c, b, qp, n_q, qt, qh, q_block, top_b, lead, tail, sel.data_ptr(), _ptr(ws),
+                                  0 if ws is None else ws.numel(), _stream())
+        if rc:
+            _check(rc)
         return sel
 
     def block_attention(self, q, kv_len, block_table, sel, q_start=None, q_block: int = 1, scale=None, max_new=None, max_kv=None,
                         out=None, want_lse: bool = False, ws=None):
         """s3_block_attention: as attention, over the blocks that sel [tiles, n_kv_heads, top_b] lists (select, or blocks of
         evidence spans).  Returns (out, lse | None)."""
-        import torch
-        b = self._batch(q.shape[0], kv_len, block_table, q_start, max_new, max_kv)
-        qa, n_q = self._rows(q), q.shape[1]
-        assert sel.is_cuda and sel.is_contiguous() and sel.dtype == torch.int32 and sel.dim() == 3
-        assert sel.shape[0] >= int(lib().s3_block_tiles(b, q_block)) and sel.shape[1] == self.n_kv_heads
-        need = int(lib().s3_block_attention_workspace(self._c, b, n_q, q_block, sel.shape[2]))
+        T, n_q, _ = q.shape
+        b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
+        qp, qt, qh = self._rows(q)
+        tiles, heads, top_b = sel.shape
+        assert sel.is_cuda and sel.is_contiguous() and sel.dtype is kv_len.dtype and heads == self.n_kv_heads
+        assert tiles >= _lib.s3_block_tiles(b, q_block)
+        need = _lib.s3_block_attention_workspace(self._c, b, n_q, q_block, top_b)
         out, lse, ws = self._out(q, out, want_lse, need, ws)
-        _check(lib().s3_block_attention(self._c, b, qa[0], n_q, qa[1], qa[2], _ptr(sel), q_block, sel.shape[2],
-                                        self.d_head ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(ws),
-                                        0 if ws is None else ws.numel(), _stream()))
+        rc = _lib.s3_block_attention(self._c, b, qp, n_q, qt, qh, sel.data_ptr(), q_block, top_b, self.scale if scale is None else scale,
+                                     out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+        if rc:
+            _check(rc)
         return out, lse
