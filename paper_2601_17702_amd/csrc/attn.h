@@ -151,14 +151,8 @@ struct AttnState {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
     }
-    // s: raw scores of NS tiles of 32 tokens, -inf where masked.  Leaves the weights in w.
-    template <int NS>
-    __device__ __forceinline__ void softmax(const kv_f32x16 (&s)[NS], float sl, vec (&w)[NS * NW]) {
-        float x = s[0][0];
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x = fmaxf(x, s[n][i]);
+    // The largest of a lane's raw scores -> what the scaled scores of both lanes' row are taken against.
+    __device__ __forceinline__ float advance(float x, float sl) {
         const float top = kv_pair_max(x) * sl;
         if (__ballot(top > m + kSlack)) {
             const float m2 = fmaxf(m, top);
@@ -170,15 +164,19 @@ struct AttnState {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[t][i] *= keep;
         }
-        const float sub = m == -INFINITY ? 0.0f : m;            // nothing seen yet: every weight is exp2(-inf)
+        return m == -INFINITY ? 0.0f : m;                       // nothing seen yet: every weight is exp2(-inf)
+    }
+    // Weights of E of the lane's 16 tokens: registers E y .. of raw scores, -inf where masked.
+    __device__ __forceinline__ vec weights(const kv_f32x16& s, int y, float sl, float sub) {
+        vec w;
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(s[n][i] * sl - sub);
-                l += e;
-                w[n * NW + i / E][i % E] = (T)e;
-            }
+        for (int e = 0; e < E; ++e) {
+            const float x = __builtin_amdgcn_exp2f(s[y * E + e] * sl - sub);
+            l += x;
+            w[e] = (T)x;
+        }
+        asm volatile("" : "+v"(l));      // summed here, not behind the products: nothing else would run beside it there
+        return w;
     }
     // A token whose values are not all finite, in a tile where some rows do not see it: zero took the place of its infinities and NaNs
     // in the product (0 * inf is NaN), and the rows that do see it get them here.  value(c): the token's channel c.

@@ -197,14 +197,20 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                 }
                 const bool masked = is_masked(a, b);
                 if (masked) {
+                    asm volatile("");                                              // stays a branch: most pieces skip it
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
                         const int t = 2 * E * (x / E) + E * half + x % E;
                         sc[0][x] = sight.sees((2 * E * (x / E) < 16 ? a.x : b.x) + (t & 15)) ? sc[0][x] : -INFINITY;
                     }
                 }
+                float x = sc[0][0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) x = fmaxf(x, sc[0][e]);
+                const float sub = st.advance(x, p.sl);
                 vec w[NW];
-                st.softmax(sc, p.sl, w);
+#pragma unroll
+                for (int y = 0; y < NW; ++y) w[y] = st.weights(sc[0], y, p.sl, sub);
                 if (masked) {
                     unsigned big = 0;
 #pragma unroll

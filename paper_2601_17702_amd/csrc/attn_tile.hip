@@ -26,7 +26,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     typedef typename KvElem<T>::vec vec;
     extern __shared__ char lds[];
     char* buf = lds;                                                  // [2][keys | values][PIECES * 16]
-    int2* runs = (int2*)(lds + 4 * PIECES * 16);                      // [kBatchRuns]: position of 16 tokens (2^30: none), page
+    int4* runs = (int4*)(lds + 4 * PIECES * 16);                      // [kBatchRuns]: bytes to 16 tokens' page and head, slot, position (2^30: none)
+    int2* spans = (int2*)(runs + kBatchRuns);                         // [kBatchRuns * 16 / KT]: a step's least and largest position
+    int* odd_step = (int*)(spans + kBatchRuns * 16 / KT);             // [2]: the step whose values in that buffer were not all finite
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int logp = p.b.log_page, P = 1 << logp;
@@ -71,27 +73,54 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
         st[r].clear();
     }
 
+    // what some row of the workgroup does not see: such steps are masked, and their values looked at
+    const int wg0 = len - n + r0 / p.G;
+    auto partly = [&](int2 span, int first_pos, int last_pos) {
+        return span.y > first_pos || span.y >= hi || (p.window && span.x <= last_pos - p.window);
+    };
+    auto span_of = [&](int t) {
+        const int2 x = spans[t];
+        return int2{__builtin_amdgcn_readfirstlane(x.x), __builtin_amdgcn_readfirstlane(x.y)};
+    };
+    // this thread's pieces: where they lie within their 16 tokens (the rest is the same for all of those)
     vec stage[2 * LOADS];
+    const char *kp[LOADS], *vp[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int x = tid + i * THREADS;
+        kp[i] = p.k + (x / KT * P + x % 16) * 16;
+        vp[i] = p.v + (x / D * E % 16 / E * D + x % D) * 16;
+    }
     auto fetch = [&](int t) {                                         // step t of the batch: into registers
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int x = tid + i * THREADS, g = x / KT, tok = x % KT;
-            const int2 r = runs[t * (KT / 16) + tok / 16];
-            const char* src = p.k + ((int64_t)max(r.y, 0) * p.n_kv + head) * page_bytes + (g * P + (r.x & (P - 1)) + (tok & 15)) * 16;
-            stage[i] = *(const vec*)src;
+            const int4 r = runs[t * (KT / 16) + (tid + i * THREADS) % KT / 16];
+            stage[i] = *(const vec*)(kp[i] + ((int64_t)(((uint64_t)(unsigned)r.y << 32) | (unsigned)r.x) + r.z * 16));
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int x = tid + i * THREADS, g = x / D, c = x % D;
-            const int2 r = runs[t * (KT / 16) + g * E / 16];
-            const char* src = p.v + ((int64_t)max(r.y, 0) * p.n_kv + head) * page_bytes + (((r.x & (P - 1)) + g * E % 16) / E * D + c) * 16;
-            // values past the end are anything: they must not meet a weight of zero as infinities
-            stage[LOADS + i] = *(const vec*)src;
-            if (r.x + 16 > hi) stage[LOADS + i] = kv_first(stage[LOADS + i], hi - r.x - g * E % 16);
+            const int4 r = runs[t * (KT / 16) + (tid + i * THREADS) / D * E / 16];
+            stage[LOADS + i] = *(const vec*)(vp[i] + ((int64_t)(((uint64_t)(unsigned)r.y << 32) | (unsigned)r.x) + r.z * (D * 16 / E)));
         }
     };
-    auto store = [&](int b) {
-        char* dst = buf + b * (2 * PIECES * 16) + tid * 16;
+    // Where some row does not see some token of the step, values that are not finite leave the buffer: their products with a weight of zero
+    // would be NaN.  The rows that do see them get them from memory, one token at a time (rare); what lies past the end is zero.
+    auto store = [&](int t) {
+        if (partly(span_of(t), wg0, hi - 1)) {
+            unsigned big = 0;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int g = (tid + i * THREADS) / D * E;
+                stage[LOADS + i] = kv_first(stage[LOADS + i], hi - runs[t * (KT / 16) + g / 16].w - g % 16);
+                big = kv_magnitude(stage[LOADS + i], big);
+            }
+            if (big >= 0x7f800000u) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) stage[LOADS + i] = kv_finite(stage[LOADS + i]);
+                odd_step[t & 1] = t;
+            }
+        }
+        char* dst = buf + (t & 1) * (2 * PIECES * 16) + tid * 16;
 #pragma unroll
         for (int i = 0; i < 2 * LOADS; ++i) *(vec*)(dst + i * THREADS * 16) = stage[i];
     };
@@ -100,6 +129,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     for (int tb = t0; tb < t1; tb += kBatch) {
         const int nb = min(kBatch, t1 - tb);
         __syncthreads();
+        if (tid < 2) odd_step[tid] = -1;
         for (int i = tid; i < nb * (KT / 16); i += THREADS) {
             int pos = 1 << 30, page = -1;
             if (LIST) {
@@ -111,7 +141,19 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
             }
             if (pos < hi) page = kv_page(p.b, s, pos >> logp);
             if (page < 0) pos = 1 << 30;
-            runs[i] = int2{pos, page};
+            const int64_t at = ((int64_t)max(page, 0) * p.n_kv + head) * page_bytes;      // no page: any memory of the cache
+            runs[i] = int4{(int)at, (int)(at >> 32), page < 0 ? 0 : pos & (P - 1), pos};
+        }
+        __syncthreads();
+        for (int i = tid; i < nb; i += THREADS) {
+            int2 span = {1 << 30, 0};
+#pragma unroll
+            for (int x = 0; x < KT / 16; ++x) {
+                const int pos = runs[i * (KT / 16) + x].w;
+                span.x = min(span.x, pos);
+                span.y = max(span.y, pos + 15);
+            }
+            spans[i] = span;
         }
         __syncthreads();
         fetch(0);
@@ -122,16 +164,10 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
             if (more) fetch(t + 1);
             const char* kb = buf + (t & 1) * (2 * PIECES * 16);
             const char* vb = kb + PIECES * 16;
-            // the tokens' positions, 16 at a time: the same in every lane
-            int pos[KT / 16], least = 1 << 30, most = 0;
-#pragma unroll
-            for (int x = 0; x < KT / 16; ++x) {
-                pos[x] = __builtin_amdgcn_readfirstlane(runs[t * (KT / 16) + x].x);
-                least = min(least, pos[x]);
-                most = max(most, pos[x] + 15);
-            }
-            if (least <= pos1) {                                      // some row of the wavefront sees some token
-                const bool masked = most > pos0 || most >= hi || (p.window && least <= pos1 - p.window);
+            const int2 span = span_of(t);
+            if (span.x <= pos1) {                                     // some row of the wavefront sees some token
+                // kAhead operands are read ahead of the products that take them (the compiler's own order waits for each)
+                constexpr int kAhead = 6, kProducts = RS * (E == 8 ? 1 : 4), DT = D / 32;
                 kv_f32x16 sc[RS][NS];
 #pragma unroll
                 for (int x = 0; x < NS; ++x) {
@@ -146,8 +182,21 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
                         for (int r = 0; r < RS; ++r) sc[r][x] = kv_mma(kf, rows[r].q[q], sc[r][x]);
                     }
                 }
-                bool odd = false;
+                auto values = [&](int y, vec (&v)[DT]) {              // operands of E tokens a lane
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) v[dt] = *(const vec*)(vb + ((2 * y + half) * D + dt * 32 + col) * 16);
+                };
+                vec v[2][DT], w[2][RS];
+                values(0, v[0]);
+                __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+                for (int i = 0; i < NS * QS; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, kProducts, 0);
+                    if (i + kAhead < NS * QS + DT) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                const bool masked = partly(span, pos0, pos1);
                 if (masked) {
+                    asm volatile("");                                 // stays a branch: most steps skip it
 #pragma unroll
                     for (int r = 0; r < RS; ++r) {
                         const AttnSight sight(rows[r].pos, hi, p.window);
@@ -156,38 +205,58 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
                                 const int tk = x * 32 + 2 * E * (i / E) + E * half + i % E;
-                                sc[r][x][i] = sight.sees(pos[(x * 32 + 2 * E * (i / E)) / 16] + (tk & 15)) ? sc[r][x][i] : -INFINITY;
+                                sc[r][x][i] = sight.sees(runs[t * (KT / 16) + (x * 32 + 2 * E * (i / E)) / 16].w + (tk & 15)) ? sc[r][x][i] : -INFINITY;
                             }
                     }
-                    unsigned big = 0;
-                    for (int i = lane; i < PIECES; i += 64) big = kv_magnitude(*(const vec*)(vb + i * 16), big);
-                    odd = __ballot(big >= 0x7f800000u) != 0;
                 }
-                vec w[RS][NS * NW];
+                float sub[RS];
 #pragma unroll
-                for (int r = 0; r < RS; ++r) st[r].softmax(sc[r], p.sl, w[r]);
+                for (int r = 0; r < RS; ++r) {
+                    float x = sc[r][0][0];
 #pragma unroll
-                for (int x = 0; x < NS; ++x)
+                    for (int y = 0; y < NS; ++y)
 #pragma unroll
-                    for (int y = 0; y < NW; ++y)
+                        for (int i = 0; i < 16; ++i) x = fmaxf(x, sc[r][y][i]);
+                    sub[r] = st[r].advance(x, p.sl);
+                }
+                // the weights and operands of the next tokens are made while these tokens' products run
 #pragma unroll
-                        for (int dt = 0; dt < D / 32; ++dt) {
-                            vec vf = *(const vec*)(vb + ((x * (32 / E) + 2 * y + half) * D + dt * 32 + col) * 16);
-                            if (odd) vf = kv_finite(vf);
+                for (int r = 0; r < RS; ++r) w[0][r] = st[r].weights(sc[r][0], 0, p.sl, sub[r]);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                            for (int r = 0; r < RS; ++r) st[r].o[dt] = kv_mma(vf, w[r][x * NW + y], st[r].o[dt]);
+                for (int y = 0; y < NS * NW; ++y) {
+                    if (y + 1 < NS * NW) {
+                        values(y + 1, v[(y + 1) & 1]);
+#pragma unroll
+                        for (int r = 0; r < RS; ++r) w[(y + 1) & 1][r] = st[r].weights(sc[r][(y + 1) / NW], (y + 1) % NW, p.sl, sub[r]);
+                    }
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int r = 0; r < RS; ++r) st[r].o[dt] = kv_mma(v[y & 1][dt], w[y & 1][r], st[r].o[dt]);
+                    if (y + 1 < NS * NW) {
+                        __builtin_amdgcn_sched_group_barrier(0x100, DT, 0);
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) {
+                            __builtin_amdgcn_sched_group_barrier(0x8, kProducts, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x402, (RS * E * 7 / 2 + DT - 1) / DT, 0);
                         }
-                if (odd)
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (partly(span, wg0, hi - 1) && odd_step[t & 1] == t)
 #pragma unroll 1
                     for (int tk = 0; tk < KT; ++tk) {
-                        const int at = runs[t * (KT / 16) + tk / 16].x + (tk & 15);
-                        const char* v = vb + tk / E * (D * 16) + tk % E * ES;
+                        const int4 r = runs[t * (KT / 16) + tk / 16];
+                        const int slot = r.z + (tk & 15);
+                        if (r.w + (tk & 15) >= hi) continue;
+                        const char* src = p.v + ((int64_t)(((uint64_t)(unsigned)r.y << 32) | (unsigned)r.x)) + slot / E * (D * 16) + slot % E * ES;
 #pragma unroll
-                        for (int r = 0; r < RS; ++r)
-                            st[r].add_nonfinite(AttnSight(rows[r].pos, hi, p.window).sees(at), [&](int c) { return (float)*(const T*)(v + c * 16); });
+                        for (int x = 0; x < RS; ++x)
+                            st[x].add_nonfinite(AttnSight(rows[x].pos, hi, p.window).sees(r.w + (tk & 15)), [&](int c) { return (float)*(const T*)(src + c * 16); });
                     }
             }
-            if (more) store((t + 1) & 1);
+            if (more) store(t + 1);
             __syncthreads();
         }
     }
@@ -278,7 +347,7 @@ int rows_of(const s3_kv_cache* c) { return c->d_head * (c->dtype == S3_BF16 ? 2 
 template <typename T, int D, bool LIST>
 int launch(const AttnArgs& p, const TileArgs& ta, hipStream_t st) {
     constexpr int RS = kSets<T, D>, W = kWaves<T, D>, ROWS = kRows<T, D>;
-    constexpr int bytes = 4 * kTokens<T, D> * D * (int)sizeof(T) + kBatchRuns * 8;
+    constexpr int bytes = 4 * kTokens<T, D> * D * (int)sizeof(T) + kBatchRuns * 16 + kBatchRuns * 16 / kTokens<T, D> * 8 + 8;
     static S3LdsOnce once;
     if (int rc = s3_allow_lds(once, (const void*)attn_tile_kernel<T, D, LIST, RS, W>, bytes)) return rc;
     const int64_t units = (int64_t)ta.tiles * p.n_kv;
