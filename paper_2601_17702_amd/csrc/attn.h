@@ -197,3 +197,26 @@ struct AttnState {
 // 1 / l, or what makes a row that saw nothing 0; its lse.
 __device__ __forceinline__ float kv_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 __device__ __forceinline__ float kv_lse(float m, float l) { return l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f; }
+// What brings sums against m (l the weights' sum) to sums against the larger m2; sums of nothing count as zero.
+__device__ __forceinline__ float kv_factor(float m, float l, float m2) {
+    return m == -INFINITY && l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(m == m2 ? 0.0f : m - m2);
+}
+
+// Lists: the runs of 16 tokens that are there move together (their order stays), -1 entries and blocks past the end take no work.
+// keep: does this thread's run stay; returns its place, and how many stay of all threads.  sums: one int per wavefront.
+template <int WAVES>
+__device__ __forceinline__ int kv_compact(bool keep, int* sums, int& total) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t b = __ballot(keep);
+    if (lane == 0) sums[wave] = __popcll(b);
+    __syncthreads();
+    int at = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        at += w < wave ? sums[w] : 0;
+        total += sums[w];
+    }
+    __syncthreads();
+    return at + __popcll(b & (((uint64_t)1 << lane) - 1));
+}

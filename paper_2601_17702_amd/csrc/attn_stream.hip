@@ -66,10 +66,11 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
     constexpr int E = KvElem<T>::E, NW = 16 / E, QS = kQSteps<D, T>, ES = (int)sizeof(T), LD = D + 4;
     typedef typename KvElem<T>::vec vec;
     extern __shared__ char lds[];
+    __shared__ int wave_sum[kWaves];
     float* sum_m = (float*)lds;                       // [kWaves][32]
     float* sum_l = sum_m + kWaves * 32;               // [kWaves][32]
-    int2* runs = (int2*)(sum_l + kWaves * 32);        // [kBatchRuns + 8]: position of 16 tokens (or beyond all), page
-    float* sum_o = (float*)(runs + kBatchRuns + 8);   // [kWaves][R][LD]
+    int2* runs = (int2*)(sum_l + kWaves * 32);        // [kBatchRuns + 16]: position of 16 tokens (or beyond all), page
+    float* sum_o = (float*)(runs + kBatchRuns + 16);   // [kWaves][R][LD]
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int logp = p.b.log_page, P = 1 << logp;
@@ -136,24 +137,31 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         const int32_t* list = LIST ? p.sel + ((int64_t)(tile0 + tile) * p.n_kv + head) * p.top : nullptr;
         const int n_list = LIST ? p.top << (logp - 4) : 0;
         for (int cb = c0; cb < c1; cb += kBatchRuns / 8) {
-            const int n = min(c1 - cb, kBatchRuns / 8) * 8;
+            int n = min(c1 - cb, kBatchRuns / 8) * 8;
             __syncthreads();                                                       // the last batch, the last tile's sums are read
-            for (int i = tid; i < n + 8; i += kThreads) {
-                int pos = 1 << 30, page = -1;
-                if (i < n) {
-                    if (LIST) {
-                        const int j = cb * 8 + i;
-                        const int blk = j < n_list ? list[j >> (logp - 4)] : -1;
-                        if (blk >= 0 && blk < p.b.max_pages) pos = (blk << logp) + (j & (P / 16 - 1)) * 16;
-                    } else {
-                        pos = part.lo + cb * kPiece + i * 16;
-                    }
-                    if (pos < hi) page = kv_page(p.b, s, pos >> logp);
-                    if (page < 0) pos = 1 << 30;
+            if (LIST) {
+                int there = 0;
+                for (int i0 = 0; i0 < n; i0 += kThreads) {
+                    const int j = cb * 8 + i0 + tid;
+                    const int blk = i0 + tid < n && j < n_list ? list[j >> (logp - 4)] : -1;
+                    const int pos = blk >= 0 && blk < p.b.max_pages ? (blk << logp) + (j & (P / 16 - 1)) * 16 : 1 << 30;
+                    const int page = pos < hi ? kv_page(p.b, s, blk) : -1;
+                    int total;
+                    const int at = kv_compact<kWaves>(page >= 0, wave_sum, total);
+                    if (page >= 0) runs[there + at] = int2{pos, page};
+                    there += total;
                 }
-                runs[i] = int2{pos, page};
+                n = (there + 7) & ~7;
+                if (tid < n + 8 - there) runs[there + tid] = int2{1 << 30, -1};
+            } else {
+                for (int i = tid; i < n + 8; i += kThreads) {
+                    int pos = i < n ? part.lo + cb * kPiece + i * 16 : 1 << 30;
+                    const int page = pos < hi ? kv_page(p.b, s, pos >> logp) : -1;
+                    runs[i] = int2{page < 0 ? 1 << 30 : pos, page};
+                }
             }
             __syncthreads();
+            if (n == 0) continue;
             const int n_sub = n / 8;
             vec kf[QS], vf[D / 32 * NW];
             int2 ra = runs[2 * wave], rb = runs[2 * wave + 1];
@@ -283,7 +291,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
                 const float mw = sum_m[w * 32 + r];
-                lsum += sum_l[w * 32 + r] * (mw == -INFINITY && sum_l[w * 32 + r] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mw == m ? 0.0f : mw - m));
+                lsum += sum_l[w * 32 + r] * kv_factor(mw, sum_l[w * 32 + r], m);
                 o += *(const kv_f32x4*)(sum_o + (w * R + r) * LD + c);
             }
             if (whole) {
@@ -306,10 +314,11 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
     }
 }
 
-// Joins the runs of the row tiles that more than one workgroup had: a workgroup per tile, head and 32 channels.
+// Joins the runs of the row tiles that more than one workgroup had: a workgroup per tile and head, 32 channels and 4 rows; eight
+// threads have a row's channels, and eight such share its runs.
 template <typename T, int D, bool LIST>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const float* slots, int R, int groups) {
-    __shared__ float part_o[kThreads][4];
+    __shared__ float part_o[kThreads][4], part_m[kThreads], part_l[kThreads];
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t total = line_length<LIST>(p);
     const int64_t per = (total + groups - 1) / groups;
@@ -347,55 +356,53 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const f
     const int r0 = LIST ? (int)want * p.qb * p.G : 0;
     const int n_rows = min(R, min(part.n, LIST ? ((int)want + 1) * p.qb : part.n) * p.G - r0);
     const int64_t stride = (int64_t)R * (D + 2);
-    const int c = blockIdx.y * 32 + (tid & 7) * 4;
-    // 8 threads have a row's 32 channels, the others of the row's share its runs
-    for (int rb = 0; rb < n_rows; rb += 4) {
-        const int r = rb + (tid >> 3 & 3), lanes_of_runs = kThreads / 32, k = tid >> 5;
-        float m = -INFINITY, l = 0.0f;
-        kv_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (r < n_rows) {
-            for (int w = w0; w <= w1; ++w) m = fmaxf(m, slots[(w * 2 + (w == w0)) * stride + R * D + r]);
-            for (int w = w0 + k; w <= w1; w += lanes_of_runs) {
-                const float* slot = slots + (w * 2 + (w == w0)) * stride;
-                const float mw = slot[R * D + r], lw = slot[R * D + R + r];
-                const float f = mw == -INFINITY && lw == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mw == m ? 0.0f : mw - m);
-                l += lw * f;
-                o += *(const kv_f32x4*)(slot + r * D + c) * f;
-            }
+    const int c = blockIdx.y * 32 + (tid & 7) * 4, r = blockIdx.z * 4 + (tid >> 3 & 3), k = tid >> 5;
+    constexpr int kShare = kThreads / 32;
+    float m = -INFINITY, l = 0.0f;
+    kv_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    // sums against m and one more's against mw, both against the larger
+    auto add = [&](float mw, float lw, kv_f32x4 ow) {
+        const float m2 = fmaxf(m, mw), a = kv_factor(m, l, m2), b = kv_factor(mw, lw, m2);
+        m = m2;
+        l = l * a + lw * b;
+        o = o * a + ow * b;
+    };
+    if (r < n_rows) {
+#pragma unroll 4
+        for (int w = w0 + k; w <= w1; w += kShare) {
+            const float* slot = slots + (w * 2 + (w == w0)) * stride;
+            add(slot[R * D + r], slot[R * D + R + r], *(const kv_f32x4*)(slot + r * D + c));
         }
-        __shared__ float part_l[kThreads];
-        part_l[tid] = l;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part_o[tid][e] = o[e];
-        __syncthreads();
-        if (k == 0 && r < n_rows) {
-#pragma unroll
-            for (int w = 1; w < kThreads / 32; ++w) {
-                l += part_l[tid + w * 32];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += part_o[tid + w * 32][e];
-            }
-            const int t = (r0 + r) / p.G;
-            const int64_t row = (int64_t)(part.first + t) * p.n_q + head * p.G + (r0 + r - t * p.G);
-            const float inv = kv_inverse(l);
-            typedef __attribute__((ext_vector_type(4))) T four;
-            *(four*)(p.out + (row * D + c) * (int)sizeof(T)) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
-            if (p.lse && c == 0) p.lse[row] = kv_lse(m, l);
-        }
-        __syncthreads();
     }
+    part_m[tid] = m;
+    part_l[tid] = l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part_o[tid][e] = o[e];
+    __syncthreads();
+    if (k || r >= n_rows) return;
+#pragma unroll
+    for (int w = 1; w < kShare; ++w) {
+        const int x = tid + w * 32;
+        add(part_m[x], part_l[x], kv_f32x4{part_o[x][0], part_o[x][1], part_o[x][2], part_o[x][3]});
+    }
+    const int t = (r0 + r) / p.G;
+    const int64_t row = (int64_t)(part.first + t) * p.n_q + head * p.G + (r0 + r - t * p.G);
+    const float inv = kv_inverse(l);
+    typedef __attribute__((ext_vector_type(4))) T four;
+    *(four*)(p.out + (row * D + c) * (int)sizeof(T)) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
+    if (p.lse && c == 0) p.lse[row] = kv_lse(m, l);
 }
 
 template <typename T, int D, bool LIST>
 int launch(const AttnArgs& p, int64_t tiles, int R, float* ws, hipStream_t st) {
     static S3LdsOnce once;
-    const int bytes = kWaves * 32 * 8 + (kBatchRuns + 8) * 8 + kWaves * R * (D + 4) * 4;
-    if (int rc = s3_allow_lds(once, (const void*)attn_stream_kernel<T, D, LIST>, kWaves * 32 * 8 + (kBatchRuns + 8) * 8 + kWaves * 32 * (D + 4) * 4)) return rc;
+    const int bytes = kWaves * 32 * 8 + (kBatchRuns + 16) * 8 + kWaves * R * (D + 4) * 4;
+    if (int rc = s3_allow_lds(once, (const void*)attn_stream_kernel<T, D, LIST>, kWaves * 32 * 8 + (kBatchRuns + 16) * 8 + kWaves * 32 * (D + 4) * 4)) return rc;
     const int64_t join = tiles * p.n_kv;
     if (join >= (int64_t)1 << 22) return s3_fail(S3_EINVAL, "attention: too many tokens in one call");
     hipLaunchKernelGGL((attn_stream_kernel<T, D, LIST>), dim3(kRunGroups), dim3(kThreads), bytes, st, p, ws, R);
     S3_HIP(hipGetLastError());
-    hipLaunchKernelGGL((attn_join_kernel<T, D, LIST>), dim3((unsigned)join, D / 32), dim3(kThreads), 0, st, p, ws, R, kRunGroups);
+    hipLaunchKernelGGL((attn_join_kernel<T, D, LIST>), dim3((unsigned)join, D / 32, (R + 3) / 4), dim3(kThreads), 0, st, p, ws, R, kRunGroups);
     S3_HIP(hipGetLastError());
     return S3_OK;
 }

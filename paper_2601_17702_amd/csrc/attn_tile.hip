@@ -25,6 +25,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     static_assert(PIECES % THREADS == 0, "every thread has as many pieces");
     typedef typename KvElem<T>::vec vec;
     extern __shared__ char lds[];
+    __shared__ int wave_sum[WAVES];
     char* buf = lds;                                                  // [2][keys | values][PIECES * 16]
     int4* runs = (int4*)(lds + 4 * PIECES * 16);                      // [kBatchRuns]: bytes to 16 tokens' page and head, slot, position (2^30: none)
     int2* spans = (int2*)(runs + kBatchRuns);                         // [kBatchRuns * 16 / KT]: a step's least and largest position
@@ -127,22 +128,33 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
 
     constexpr int kBatch = kBatchRuns / (KT / 16);                    // steps whose pages are known at a time
     for (int tb = t0; tb < t1; tb += kBatch) {
-        const int nb = min(kBatch, t1 - tb);
+        int nb = min(kBatch, t1 - tb);
         __syncthreads();
         if (tid < 2) odd_step[tid] = -1;
-        for (int i = tid; i < nb * (KT / 16); i += THREADS) {
-            int pos = 1 << 30, page = -1;
-            if (LIST) {
-                const int x = tb * (KT / 16) + i;
-                const int blk = x < n_list ? list[x >> (logp - 4)] : -1;
-                if (blk >= 0 && blk < p.b.max_pages) pos = (blk << logp) + (x & (P / 16 - 1)) * 16;
-            } else {
-                pos = lo + tb * KT + i * 16;
-            }
-            if (pos < hi) page = kv_page(p.b, s, pos >> logp);
-            if (page < 0) pos = 1 << 30;
+        auto put = [&](int i, int pos, int page) {
             const int64_t at = ((int64_t)max(page, 0) * p.n_kv + head) * page_bytes;      // no page: any memory of the cache
-            runs[i] = int4{(int)at, (int)(at >> 32), page < 0 ? 0 : pos & (P - 1), pos};
+            runs[i] = int4{(int)at, (int)(at >> 32), page < 0 ? 0 : pos & (P - 1), page < 0 ? 1 << 30 : pos};
+        };
+        if (LIST) {
+            int there = 0;
+            for (int i0 = 0; i0 < nb * (KT / 16); i0 += THREADS) {
+                const int x = tb * (KT / 16) + i0 + tid;
+                const int blk = i0 + tid < nb * (KT / 16) && x < n_list ? list[x >> (logp - 4)] : -1;
+                const int pos = blk >= 0 && blk < p.b.max_pages ? (blk << logp) + (x & (P / 16 - 1)) * 16 : 1 << 30;
+                const int page = pos < hi ? kv_page(p.b, s, blk) : -1;
+                int total;
+                const int at = kv_compact<WAVES>(page >= 0, wave_sum, total);
+                if (page >= 0) put(there + at, pos, page);
+                there += total;
+            }
+            nb = (there + KT / 16 - 1) / (KT / 16);
+            if (tid < nb * (KT / 16) - there) put(there + tid, 1 << 30, -1);
+            if (nb == 0) continue;
+        } else {
+            for (int i = tid; i < nb * (KT / 16); i += THREADS) {
+                const int pos = lo + tb * KT + i * 16;
+                put(i, pos, pos < hi ? kv_page(p.b, s, pos >> logp) : -1);
+            }
         }
         __syncthreads();
         for (int i = tid; i < nb; i += THREADS) {
@@ -325,7 +337,7 @@ __global__ __launch_bounds__(256) void attn_tile_join_kernel(AttnArgs p, TileArg
     for (int w = 0; w < ta.n_split; ++w) m = fmaxf(m, slots[w * stride + ROWS * D + row]);
     for (int w = 0; w < ta.n_split; ++w) {
         const float mw = slots[w * stride + ROWS * D + row], lw = slots[w * stride + ROWS * D + ROWS + row];
-        const float f = mw == -INFINITY && lw == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(mw == m ? 0.0f : mw - m);
+        const float f = kv_factor(mw, lw, m);
         l += lw * f;
         o += *(const kv_f32x4*)(slots + w * stride + row * D + c) * f;
     }

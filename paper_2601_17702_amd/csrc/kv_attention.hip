@@ -28,11 +28,13 @@ struct Plan {
     int64_t few_tiles, many_tiles;
     size_t few_ws, many_ws;
     size_t bytes() const { return few_ws + many_ws; }
-    Plan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b) {
+    Plan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b, int window) {
         G = n_q / c->n_kv_heads;
         qb = min(q_block, max(b->n_tokens, 1));
         const int64_t most = (int64_t)(q_block ? qb : min(max(b->max_new, 1), max(b->n_tokens, 1))) * G;
-        few = most <= 32 || (!q_block && b->n_seq > 1);
+        // no sequence is a short one if even the others at their longest leave more than 32 rows for it
+        const bool all_long = b->n_tokens > (int64_t)(b->n_seq - 1) * b->max_new + 32 / G;
+        few = most <= 32 || (!q_block && !all_long);
         many = most > 32;
         R = (int)min(most, (int64_t)32);
         few_tiles = q_block ? s3_block_tiles(b, q_block) : b->n_seq;
@@ -41,8 +43,10 @@ struct Plan {
         per_q = !q_block || !many ? 1 : (int)((most + rows - 1) / rows);
         many_tiles = !many ? 0 : q_block ? s3_block_tiles(b, q_block) * per_q
                                          : ((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * (rows - 1)) / rows;
-        n_split = many ? s3_attn_tile_split(c, many_tiles * c->n_kv_heads, q_block ? (int64_t)top_b * c->page_size : b->max_kv) : 1;
-        many_ws = s3_attn_tile_workspace(c, many_tiles * c->n_kv_heads, n_split);
+        const int64_t units = many_tiles * c->n_kv_heads, tokens = q_block ? (int64_t)top_b * c->page_size : b->max_kv;
+        n_split = many ? s3_attn_tile_split(c, units, tokens) : 1;
+        many_ws = s3_attn_tile_workspace(c, units, n_split);              // for any window
+        if (many && window) n_split = min(n_split, s3_attn_tile_split(c, units, min(tokens, (int64_t)window + rows / G)));
     }
 };
 
@@ -62,7 +66,7 @@ bool shapes_ok(const s3_kv_cache* c, const s3_kv_batch* b, int n_q) {
 }  // namespace
 
 extern "C" size_t s3_paged_attention_workspace(const s3_kv_cache* c, const s3_kv_batch* b, int n_q) {
-    return shapes_ok(c, b, n_q) ? Plan(c, b, n_q, 0, 0).bytes() : 0;
+    return shapes_ok(c, b, n_q) ? Plan(c, b, n_q, 0, 0, 0).bytes() : 0;
 }
 
 extern "C" int s3_paged_attention(const s3_kv_cache* c, const s3_kv_batch* b, const void* q, int n_q, int64_t q_ts, int64_t q_hs,
@@ -70,7 +74,7 @@ extern "C" int s3_paged_attention(const s3_kv_cache* c, const s3_kv_batch* b, co
     const char* fn = "s3_paged_attention";
     if (window < 0) return s3_fail(S3_EINVAL, "%s: window %d", fn, window);
     if (int rc = check(fn, c, b, q, n_q, q_ts, q_hs, scale, out)) return rc < 0 ? rc : S3_OK;
-    const Plan plan(c, b, n_q, 0, 0);
+    const Plan plan(c, b, n_q, 0, 0, window);
     if (int rc = check_ws(fn, ws, ws_bytes, plan.bytes())) return rc;
     const int es = c->dtype == S3_BF16 ? 2 : 4;
     AttnArgs p{s3_kv_batch_args(c, b), (const char*)q, (char*)out, lse, (const char*)c->k, (const char*)c->v, nullptr, q_ts * es,
@@ -83,7 +87,7 @@ extern "C" int64_t s3_block_tiles(const s3_kv_batch* b, int q_block) {
 }
 
 extern "C" size_t s3_block_attention_workspace(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b) {
-    return shapes_ok(c, b, n_q) && q_block >= 1 && top_b >= 1 ? Plan(c, b, n_q, q_block, top_b).bytes() : 0;
+    return shapes_ok(c, b, n_q) && q_block >= 1 && top_b >= 1 ? Plan(c, b, n_q, q_block, top_b, 0).bytes() : 0;
 }
 
 extern "C" int s3_block_attention(const s3_kv_cache* c, const s3_kv_batch* b, const void* q, int n_q, int64_t q_ts, int64_t q_hs,
@@ -93,7 +97,7 @@ extern "C" int s3_block_attention(const s3_kv_cache* c, const s3_kv_batch* b, co
     if (q_block < 1 || top_b < 1 || q_block > 1 << 20 || top_b > 4096) return s3_fail(S3_EINVAL, "%s: q_block %d, top_b %d", fn, q_block, top_b);
     if (int rc = check(fn, c, b, q, n_q, q_ts, q_hs, scale, out)) return rc < 0 ? rc : S3_OK;
     if (!sel) return s3_fail(S3_EINVAL, "%s: null sel", fn);
-    const Plan plan(c, b, n_q, q_block, top_b);
+    const Plan plan(c, b, n_q, q_block, top_b, 0);
     if (int rc = check_ws(fn, ws, ws_bytes, plan.bytes())) return rc;
     const int es = c->dtype == S3_BF16 ? 2 : 4;
     AttnArgs p{s3_kv_batch_args(c, b), (const char*)q, (char*)out, lse, (const char*)c->k, (const char*)c->v, sel, q_ts * es,
