@@ -35,9 +35,9 @@ struct AttnArgs {
     const int32_t* sel;       // block lists, or null: all blocks
     int64_t q_ts, q_hs;       // bytes
     int n_kv, G, n_q, window;
-    int qb, top, per_q;       // lists: tokens a tile, entries, tiles of 32 rows a tile of queries
+    int qb, top, per_q;       // lists: tokens a tile, entries, row tiles a tile of queries
     float sl;                 // scale * log2(e)
-    int few;                  // sequences of at most 32 rows are another launch's
+    int few;                  // sequences of at most this many rows are the streaming kernel's
 };
 
 // Largest over the two lanes that share a row; their sum.  The swap hands every lane both halves' values.

@@ -34,15 +34,28 @@ __device__ __forceinline__ Part part_of(const AttnArgs& p, int s) {
     kv_seq(p.b, s, r.first, r.n, r.len);
     r.lo = 0;
     if (LIST) {
-        r.tiles = (r.n + p.qb - 1) / p.qb;
+        r.tiles = (r.n + p.qb - 1) / p.qb * p.per_q;
         r.pieces = ((p.top << p.b.log_page) + kPiece - 1) / kPiece;
     } else {
-        r.tiles = r.n > 0 && r.n * p.G <= 32 ? 1 : 0;
+        r.tiles = r.n * p.G <= p.few ? (r.n * p.G + 31) / 32 : 0;
         if (p.window) r.lo = max(0, r.len - r.n - p.window + 1) & ~31;
         const int hi = min(r.len, kv_blocks(p.b, r.len) << p.b.log_page);
         r.pieces = (max(hi - r.lo, 1) + kPiece - 1) / kPiece;         // one at least: rows that see nothing are written, too
     }
     return r;
+}
+
+// Rows of a tile: the first, and the end.
+template <bool LIST>
+__device__ __forceinline__ void rows_of(const AttnArgs& p, const Part& part, int tile, int& r0, int& r_end) {
+    if (LIST) {
+        const int qt = tile / p.per_q;
+        r0 = qt * p.qb * p.G + (tile - qt * p.per_q) * 32;
+        r_end = min(min(part.n, (qt + 1) * p.qb) * p.G, r0 + 32);
+    } else {
+        r0 = tile * 32;
+        r_end = min(part.n * p.G, r0 + 32);
+    }
 }
 
 // The line's length and equal runs of it.
@@ -125,16 +138,16 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         const int tile = (int)(u / p.n_kv), head = (int)(u % p.n_kv);
         const int c1 = (int)min((int64_t)part.pieces, c0 + (end - at));
 
-        const int r0 = LIST ? tile * p.qb * p.G : 0;
-        const int r_end = min(part.n, LIST ? (tile + 1) * p.qb : part.n) * p.G;
+        int r0, r_end;
+        rows_of<LIST>(p, part, tile, r0, r_end);
         AttnRows<T, D> rows;
         rows.load(p, head, part.first, part.n, part.len, r0 + col, r_end);
         AttnState<T, D> st;
         st.clear();
         const int pos0 = part.len - part.n + r0 / p.G;                            // the first row's position, and the last one's
-        const int hi = min(part.len - part.n + r_end / p.G, kv_blocks(p.b, part.len) << logp);
+        const int hi = min(part.len - part.n + (r_end - 1) / p.G + 1, kv_blocks(p.b, part.len) << logp);
         const AttnSight sight(rows.pos, hi, p.window);
-        const int32_t* list = LIST ? p.sel + ((int64_t)(tile0 + tile) * p.n_kv + head) * p.top : nullptr;
+        const int32_t* list = LIST ? p.sel + ((int64_t)((tile0 + tile) / p.per_q) * p.n_kv + head) * p.top : nullptr;
         const int n_list = LIST ? p.top << (logp - 4) : 0;
         for (int cb = c0; cb < c1; cb += kBatchRuns / 8) {
             int n = min(c1 - cb, kBatchRuns / 8) * 8;
@@ -314,8 +327,8 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
     }
 }
 
-// Joins the runs of the row tiles that more than one workgroup had: a workgroup per tile and head, 32 channels and 4 rows; eight
-// threads have a row's channels, and eight such share its runs.
+// Joins the runs of the row tiles that more than one workgroup had: workgroups per tile and head that take
+// 32 channels of 4 rows at a time; eight threads have a row's channels, and eight such share its runs.
 template <typename T, int D, bool LIST>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const float* slots, int R, int groups) {
     __shared__ float part_o[kThreads][4], part_m[kThreads], part_l[kThreads];
@@ -353,44 +366,50 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const f
     const int64_t a = run + (want * p.n_kv + head) * part.pieces, b = a + part.pieces;
     const int w0 = (int)(a / per), w1 = (int)((b - 1) / per);
     if (w0 == w1) return;
-    const int r0 = LIST ? (int)want * p.qb * p.G : 0;
-    const int n_rows = min(R, min(part.n, LIST ? ((int)want + 1) * p.qb : part.n) * p.G - r0);
+    int r0, r_end;
+    rows_of<LIST>(p, part, (int)want, r0, r_end);
+    const int n_rows = min(R, r_end - r0);
     const int64_t stride = (int64_t)R * (D + 2);
-    const int c = blockIdx.y * 32 + (tid & 7) * 4, r = blockIdx.z * 4 + (tid >> 3 & 3), k = tid >> 5;
+    const int k = tid >> 5;
     constexpr int kShare = kThreads / 32;
-    float m = -INFINITY, l = 0.0f;
-    kv_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    // sums against m and one more's against mw, both against the larger
-    auto add = [&](float mw, float lw, kv_f32x4 ow) {
-        const float m2 = fmaxf(m, mw), a = kv_factor(m, l, m2), b = kv_factor(mw, lw, m2);
-        m = m2;
-        l = l * a + lw * b;
-        o = o * a + ow * b;
-    };
-    if (r < n_rows) {
+    for (int x = blockIdx.y; x < (n_rows + 3) / 4 * (D / 32); x += gridDim.y) {
+        const int c = x % (D / 32) * 32 + (tid & 7) * 4, r = x / (D / 32) * 4 + (tid >> 3 & 3);
+        float m = -INFINITY, l = 0.0f;
+        kv_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        // sums against m and one more's against mw, both against the larger
+        auto add = [&](float mw, float lw, kv_f32x4 ow) {
+            const float m2 = fmaxf(m, mw), a = kv_factor(m, l, m2), b = kv_factor(mw, lw, m2);
+            m = m2;
+            l = l * a + lw * b;
+            o = o * a + ow * b;
+        };
+        if (r < n_rows) {
 #pragma unroll 4
-        for (int w = w0 + k; w <= w1; w += kShare) {
-            const float* slot = slots + (w * 2 + (w == w0)) * stride;
-            add(slot[R * D + r], slot[R * D + R + r], *(const kv_f32x4*)(slot + r * D + c));
+            for (int w = w0 + k; w <= w1; w += kShare) {
+                const float* slot = slots + (w * 2 + (w == w0)) * stride;
+                add(slot[R * D + r], slot[R * D + R + r], *(const kv_f32x4*)(slot + r * D + c));
+            }
         }
-    }
-    part_m[tid] = m;
-    part_l[tid] = l;
+        part_m[tid] = m;
+        part_l[tid] = l;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) part_o[tid][e] = o[e];
-    __syncthreads();
-    if (k || r >= n_rows) return;
+        for (int e = 0; e < 4; ++e) part_o[tid][e] = o[e];
+        __syncthreads();
+        if (k == 0 && r < n_rows) {
 #pragma unroll
-    for (int w = 1; w < kShare; ++w) {
-        const int x = tid + w * 32;
-        add(part_m[x], part_l[x], kv_f32x4{part_o[x][0], part_o[x][1], part_o[x][2], part_o[x][3]});
+            for (int w = 1; w < kShare; ++w) {
+                const int y = tid + w * 32;
+                add(part_m[y], part_l[y], kv_f32x4{part_o[y][0], part_o[y][1], part_o[y][2], part_o[y][3]});
+            }
+            const int t = (r0 + r) / p.G;
+            const int64_t row = (int64_t)(part.first + t) * p.n_q + head * p.G + (r0 + r - t * p.G);
+            const float inv = kv_inverse(l);
+            typedef __attribute__((ext_vector_type(4))) T four;
+            *(four*)(p.out + (row * D + c) * (int)sizeof(T)) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
+            if (p.lse && c == 0) p.lse[row] = kv_lse(m, l);
+        }
+        __syncthreads();
     }
-    const int t = (r0 + r) / p.G;
-    const int64_t row = (int64_t)(part.first + t) * p.n_q + head * p.G + (r0 + r - t * p.G);
-    const float inv = kv_inverse(l);
-    typedef __attribute__((ext_vector_type(4))) T four;
-    *(four*)(p.out + (row * D + c) * (int)sizeof(T)) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
-    if (p.lse && c == 0) p.lse[row] = kv_lse(m, l);
 }
 
 template <typename T, int D, bool LIST>
@@ -402,7 +421,7 @@ int launch(const AttnArgs& p, int64_t tiles, int R, float* ws, hipStream_t st) {
     if (join >= (int64_t)1 << 22) return s3_fail(S3_EINVAL, "attention: too many tokens in one call");
     hipLaunchKernelGGL((attn_stream_kernel<T, D, LIST>), dim3(kRunGroups), dim3(kThreads), bytes, st, p, ws, R);
     S3_HIP(hipGetLastError());
-    hipLaunchKernelGGL((attn_join_kernel<T, D, LIST>), dim3((unsigned)join, D / 32, (R + 3) / 4), dim3(kThreads), 0, st, p, ws, R, kRunGroups);
+    hipLaunchKernelGGL((attn_join_kernel<T, D, LIST>), dim3((unsigned)join, (unsigned)max((int64_t)1, min(4096 / join, (int64_t)(D / 32 * ((R + 3) / 4))))), dim3(kThreads), 0, st, p, ws, R, kRunGroups);
     S3_HIP(hipGetLastError());
     return S3_OK;
 }

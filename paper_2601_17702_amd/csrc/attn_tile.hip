@@ -41,7 +41,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     auto count = [&](int q) {
         int first, n, len;
         kv_seq(p.b, q, first, n, len);
-        return LIST ? (n + p.qb - 1) / p.qb * p.per_q : p.few && n * p.G <= 32 ? 0 : (n * p.G + ROWS - 1) / ROWS;
+        return LIST ? (n + p.qb - 1) / p.qb * p.per_q : n * p.G <= p.few ? 0 : (n * p.G + ROWS - 1) / ROWS;
     };
     int s, j;
     if (!kv_find(p.b.n_seq, tile, count, s, j)) return;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256) void attn_tile_join_kernel(AttnArgs p, TileArg
     auto count = [&](int q) {
         int first, n, len;
         kv_seq(p.b, q, first, n, len);
-        return LIST ? (n + p.qb - 1) / p.qb * p.per_q : p.few && n * p.G <= 32 ? 0 : (n * p.G + ROWS - 1) / ROWS;
+        return LIST ? (n + p.qb - 1) / p.qb * p.per_q : n * p.G <= p.few ? 0 : (n * p.G + ROWS - 1) / ROWS;
     };
     int s, j;
     if (!kv_find(p.b.n_seq, tile, count, s, j)) return;

@@ -21,7 +21,8 @@ int check_ws(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
 }
 
 // How a call is shared out: rows of one sequence, or of one tile of listed blocks, are the streaming kernel's where they are at
-// most 32 and the tiled kernel's else.
+// most kFewRows and the tiled kernel's else.
+constexpr int kFewRows = 32;
 struct Plan {
     int G, R, qb, per_q, n_split;
     bool few, many;
@@ -32,15 +33,15 @@ struct Plan {
         G = n_q / c->n_kv_heads;
         qb = min(q_block, max(b->n_tokens, 1));
         const int64_t most = (int64_t)(q_block ? qb : min(max(b->max_new, 1), max(b->n_tokens, 1))) * G;
-        // no sequence is a short one if even the others at their longest leave more than 32 rows for it
-        const bool all_long = b->n_tokens > (int64_t)(b->n_seq - 1) * b->max_new + 32 / G;
-        few = most <= 32 || (!q_block && !all_long);
-        many = most > 32;
+        // no sequence is a short one if even the others at their longest leave more rows for it
+        const bool all_long = b->n_tokens > (int64_t)(b->n_seq - 1) * b->max_new + kFewRows / G;
+        few = most <= kFewRows || (!q_block && !all_long);
+        many = most > kFewRows;
         R = (int)min(most, (int64_t)32);
-        few_tiles = q_block ? s3_block_tiles(b, q_block) : b->n_seq;
         few_ws = few ? s3_attn_stream_workspace(c->d_head, R) : 0;
         const int rows = s3_attn_tile_rows(c);
-        per_q = !q_block || !many ? 1 : (int)((most + rows - 1) / rows);
+        per_q = !q_block ? 1 : (int)((most + (many ? rows : 32) - 1) / (many ? rows : 32));
+        few_tiles = q_block ? s3_block_tiles(b, q_block) * per_q : min(((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * 31) / 32, (int64_t)b->n_seq * (kFewRows / 32));
         many_tiles = !many ? 0 : q_block ? s3_block_tiles(b, q_block) * per_q
                                          : ((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * (rows - 1)) / rows;
         const int64_t units = many_tiles * c->n_kv_heads, tokens = q_block ? (int64_t)top_b * c->page_size : b->max_kv;
@@ -51,7 +52,7 @@ struct Plan {
 };
 
 int run(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b, AttnArgs p, const Plan& plan, void* ws, hipStream_t st) {
-    p.few = plan.few && plan.many;
+    p.few = plan.few ? kFewRows : 0;
     p.qb = plan.qb;
     p.per_q = plan.per_q;
     if (plan.few)
