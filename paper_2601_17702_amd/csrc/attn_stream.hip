@@ -176,23 +176,25 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
             __syncthreads();
             if (n == 0) continue;
             const int n_sub = n / 8;
-            vec kf[QS], vf[D / 32 * NW];
+            // keys and values in VC parts of the channels: all of them ahead, or (fp32, 256 channels) only the first, as far as registers go
+            constexpr int VC = D * ES > 512 ? 2 : 1, DC = D / 32 / VC, QC = QS / VC;
+            vec kf[QC], vf[DC * NW];
             int2 ra = runs[2 * wave], rb = runs[2 * wave + 1];
-            auto load_k = [&]() {
+            auto load_k = [&](int2 a, int2 b, int part) {
                 const int tk = kv_token<T>(col);
-                const int2 r = tk < 16 ? ra : rb;
-                const char* k = p.k + ((int64_t)max(r.y, 0) * p.n_kv + head) * page_bytes + ((r.y < 0 ? 0 : r.x & (P - 1)) + (tk & 15) + half * P) * 16;
+                const int2 r = tk < 16 ? a : b;
+                const char* k = p.k + ((int64_t)max(r.y, 0) * p.n_kv + head) * page_bytes + ((r.y < 0 ? 0 : r.x & (P - 1)) + (tk & 15) + half * P) * 16 + part * (QC * 32) * P;
 #pragma unroll
-                for (int q = 0; q < QS; ++q) kf[q] = *(const vec*)(k + q * 32 * P);
+                for (int q = 0; q < QC; ++q) kf[q] = *(const vec*)(k + q * 32 * P);
             };
-            auto load_v = [&](int2 a, int2 b) {
+            auto load_v = [&](int2 a, int2 b, int part) {
 #pragma unroll
                 for (int y = 0; y < NW; ++y) {
                     const int t = E * (2 * y + half);                              // first of this lane's E tokens: in one run for all lanes
                     const int2 r = 2 * E * y < 16 ? a : b;
-                    const char* v = p.v + ((int64_t)max(r.y, 0) * p.n_kv + head) * page_bytes + ((r.y < 0 ? 0 : r.x & (P - 1)) + (t & 15)) / E * (D * 16) + col * 16;
+                    const char* v = p.v + ((int64_t)max(r.y, 0) * p.n_kv + head) * page_bytes + ((r.y < 0 ? 0 : r.x & (P - 1)) + (t & 15)) / E * (D * 16) + col * 16 + part * (DC * 512);
 #pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt) vf[dt * NW + y] = *(const vec*)(v + dt * 512);
+                    for (int dt = 0; dt < DC; ++dt) vf[dt * NW + y] = *(const vec*)(v + dt * 512);
                 }
             };
             // some row does not see some token of the 32
@@ -201,20 +203,28 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                 return far > pos0 || far >= hi || (p.window && min(a.x, b.x) <= hi - 1 - p.window);
             };
             bool odd = false;
-            load_k();
-            load_v(ra, rb);
+            load_k(ra, rb, 0);
+            load_v(ra, rb, 0);
             for (int i = 0; i < n_sub; ++i) {
                 const int2 a = ra, b = rb;
                 kv_f32x16 sc[1];
 #pragma unroll
                 for (int x = 0; x < 16; ++x) sc[0][x] = 0.0f;
 #pragma unroll
-                for (int q = 0; q < QS; ++q) sc[0] = kv_mma(kf[q], rows.q[q], sc[0]);
+                for (int part = 0; part < VC; ++part) {
+                    if (part) {
+                        load_k(a, b, part);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int q = 0; q < QC; ++q) sc[0] = kv_mma(kf[q], rows.q[part * QC + q], sc[0]);
+                    if (VC > 1) __builtin_amdgcn_sched_barrier(0);
+                }
                 const bool more = i + 1 < n_sub;
                 if (more) {
                     ra = runs[(i + 1) * 8 + 2 * wave];
                     rb = runs[(i + 1) * 8 + 2 * wave + 1];
-                    load_k();
+                    load_k(ra, rb, 0);
                 }
                 const bool masked = is_masked(a, b);
                 if (masked) {
@@ -232,28 +242,35 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                 vec w[NW];
 #pragma unroll
                 for (int y = 0; y < NW; ++y) w[y] = st.weights(sc[0], y, p.sl, sub);
-                if (masked) {
-                    unsigned big = 0;
 #pragma unroll
-                    for (int y = 0; y < NW; ++y) {
-                        const int n = hi - (2 * E * y < 16 ? a.x : b.x) - (E * (2 * y + half) & 15);
+                for (int part = 0; part < VC; ++part) {
+                    if (part) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        load_v(a, b, part);
+                    }
+                    if (masked) {
+                        unsigned big = 0;
 #pragma unroll
-                        for (int dt = 0; dt < D / 32; ++dt) {
-                            vf[dt * NW + y] = kv_first(vf[dt * NW + y], n);
-                            big = kv_magnitude(vf[dt * NW + y], big);
+                        for (int y = 0; y < NW; ++y) {
+                            const int n = hi - (2 * E * y < 16 ? a.x : b.x) - (E * (2 * y + half) & 15);
+#pragma unroll
+                            for (int dt = 0; dt < DC; ++dt) {
+                                vf[dt * NW + y] = kv_first(vf[dt * NW + y], n);
+                                big = kv_magnitude(vf[dt * NW + y], big);
+                            }
+                        }
+                        if (__ballot(big >= 0x7f800000u)) {
+                            odd = true;
+#pragma unroll
+                            for (int y = 0; y < DC * NW; ++y) vf[y] = kv_finite(vf[y]);
                         }
                     }
-                    if (__ballot(big >= 0x7f800000u)) {
-                        odd = true;
 #pragma unroll
-                        for (int y = 0; y < D / 32 * NW; ++y) vf[y] = kv_finite(vf[y]);
-                    }
+                    for (int dt = 0; dt < DC; ++dt)
+#pragma unroll
+                        for (int y = 0; y < NW; ++y) st.o[part * DC + dt] = kv_mma(vf[dt * NW + y], w[y], st.o[part * DC + dt]);
                 }
-#pragma unroll
-                for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                    for (int y = 0; y < NW; ++y) st.o[dt] = kv_mma(vf[dt * NW + y], w[y], st.o[dt]);
-                if (more) load_v(ra, rb);
+                if (more) load_v(ra, rb, 0);
             }
             if (odd)
                 for (int i = 0; i < n_sub; ++i) {
