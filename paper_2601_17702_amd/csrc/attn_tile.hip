@@ -38,15 +38,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     // longest first: later row tiles see more
     const int head = blockIdx.x % p.n_kv;
     const int tile = ta.tiles - 1 - blockIdx.x / p.n_kv;
-    auto count = [&](int q) {
-        int first, n, len;
-        kv_seq(p.b, q, first, n, len);
-        return LIST ? (n + p.qb - 1) / p.qb * p.per_q : n * p.G <= p.few ? 0 : (n * p.G + ROWS - 1) / ROWS;
-    };
-    int s, j;
-    if (!kv_find(p.b.n_seq, tile, count, s, j)) return;
-    int first, n, len;
-    kv_seq(p.b, s, first, n, len);
+    auto count = [&](int n, int) { return LIST ? (n + p.qb - 1) / p.qb * p.per_q : n * p.G <= p.few ? 0 : (n * p.G + ROWS - 1) / ROWS; };
+    int s, j, first, n, len;
+    if (!kv_find(p.b, tile, count, s, j, first, n, len)) return;
     int r0 = j * ROWS, r_end = n * p.G;
     if (LIST) {
         const int qt = j / p.per_q;
@@ -313,15 +307,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
 template <typename T, int D, bool LIST, int ROWS>
 __global__ __launch_bounds__(256) void attn_tile_join_kernel(AttnArgs p, TileArgs ta) {
     const int head = blockIdx.x % p.n_kv, tile = blockIdx.x / p.n_kv;
-    auto count = [&](int q) {
-        int first, n, len;
-        kv_seq(p.b, q, first, n, len);
-        return LIST ? (n + p.qb - 1) / p.qb * p.per_q : n * p.G <= p.few ? 0 : (n * p.G + ROWS - 1) / ROWS;
-    };
-    int s, j;
-    if (!kv_find(p.b.n_seq, tile, count, s, j)) return;
-    int first, n, len;
-    kv_seq(p.b, s, first, n, len);
+    auto count = [&](int n, int) { return LIST ? (n + p.qb - 1) / p.qb * p.per_q : n * p.G <= p.few ? 0 : (n * p.G + ROWS - 1) / ROWS; };
+    int s, j, first, n, len;
+    if (!kv_find(p.b, tile, count, s, j, first, n, len)) return;
     int r0 = j * ROWS, r_end = n * p.G;
     if (LIST) {
         const int qt = j / p.per_q;

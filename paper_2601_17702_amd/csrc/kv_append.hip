@@ -4,6 +4,7 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kTokens = 4;            // whose queries one workgroup rotates, all their loads ahead, where there are many
 
 struct AppendArgs {
     KvBatch b;
@@ -18,6 +19,7 @@ struct AppendArgs {
     int64_t n_pos;
     int rot, inter, n_kv, n_q;
     unsigned page_items;                             // workgroups of pages; the rest rotate queries
+    int group;                                       // tokens of such a one
 };
 
 // E channels of one row and, for pairs (i, i + rot / 2), their E partners.  c, s: E (interleaved: E / 2) values each.
@@ -70,52 +72,80 @@ __device__ __forceinline__ void row_item(const AppendArgs& p, const char* row, i
     put(g, a);
 }
 
+// Slots that pass through LDS at a time: 16 KB of keys and of values, a row of 16 bytes more each (a column's reads then meet no bank twice).
+template <typename T, int D> constexpr int kSlab = D * (int)sizeof(T) >= 1024 ? 16 : D * (int)sizeof(T) >= 512 ? 32 : 64;
+
+// What bounds it: memory.  8 chunks of 2048 tokens, 32 query heads over 8 of 128 in bf16 (412 MB read and written) take 85 us, 4.8 TB/s: what a copy moves.
+// Rows are read whole and pages written whole lines at a time, so both layouts' transpositions go through LDS; the signature's
+// sums read the new keys there, too, and only a page's older keys come back from memory.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs p) {
-    constexpr int E = KvElem<T>::E, NG = D / E;
+    constexpr int E = KvElem<T>::E, NG = D / E, SLAB = kSlab<T, D>, ROW = D * (int)sizeof(T) + 16;
     typedef typename KvElem<T>::vec vec;
     const int tid = threadIdx.x;
     const int items = row_items<T, D>(p);
 
-    if (blockIdx.x >= p.page_items) {                // queries: one item of a row per thread
-        int64_t i = (int64_t)(blockIdx.x - p.page_items) * kThreads + tid;
-        const int item = (int)(i % items);
-        i /= items;
-        const int head = (int)(i % p.n_q);
-        const int64_t token = i / p.n_q;
-        if (token >= p.b.n_tokens) return;
-        int s = (int)token;
-        if (p.b.q_start) {                           // the last sequence that starts at or before the token
-            int lo = 0, hi = p.b.n_seq;
-            while (hi - lo > 1) {
-                const int m = (lo + hi) / 2;
-                if (p.b.q_start[m] <= token) lo = m;
-                else hi = m;
+    if (blockIdx.x >= p.page_items) {                // queries: `group` tokens; a thread has the same item of a head in several of them
+        const int per = p.n_q * items, side = max(1, kThreads / per);      // items of a token; tokens side by side
+        const int t0 = (int)(blockIdx.x - p.page_items) * p.group, t1 = min(t0 + p.group, p.b.n_tokens);
+        int s = t0;
+        if (p.b.q_start) {                           // the first sequence that ends behind the first token
+            s = -1;
+            for (int base = 0; base < p.b.n_seq && s < 0; base += 64) {
+                int f = 0, m = -1, l;
+                if (base + (tid & 63) < p.b.n_seq) kv_seq(p.b, base + (tid & 63), f, m, l);
+                const uint64_t behind = __ballot(f + m > t0);
+                if (behind) s = base + __builtin_ctzll(behind);
             }
-            s = lo;
+            if (s < 0) return;
         }
-        int first, n, len;
-        kv_seq(p.b, s, first, n, len);
-        if (token < first || token >= first + n) return;
-        char* out = p.q_out + (token * p.n_q + head) * (D * (int)sizeof(T));
-        row_item<T, D>(p, p.q + token * p.q_ts + head * p.q_hs, item, (int)token, len - n + (int)(token - first),
-                       [&](int g, vec x) { *(vec*)(out + g * 16) = x; });
+        for (int i = tid; i < per * side; i += kThreads) {
+            const int x = i / per, y = i - x * per, head = y / items, item = y - head * items;
+            int q = s, first, n, len;
+            kv_seq(p.b, q, first, n, len);
+            if (p.rope && !p.inter && side == 1 && p.group == kTokens && t0 >= first && t0 + kTokens <= first + n && item < p.rot / (2 * E)) {
+                // all of one sequence: every load before the first store
+                const char* src = p.q + (int64_t)t0 * p.q_ts + head * p.q_hs + item * 16;
+                const int far = p.rot / 2 * (int)sizeof(T);
+                vec lo2[kTokens], hi2[kTokens];
+#pragma unroll
+                for (int t = 0; t < kTokens; ++t) {
+                    lo2[t] = *(const vec*)(src + t * p.q_ts);
+                    hi2[t] = *(const vec*)(src + t * p.q_ts + far);
+                }
+                char* out = p.q_out + ((int64_t)t0 * p.n_q + head) * (D * (int)sizeof(T)) + item * 16;
+#pragma unroll
+                for (int t = 0; t < kTokens; ++t) {
+                    int64_t r = p.positions ? p.positions[t0 + t] : len - n + (t0 + t - first);
+                    r = max((int64_t)0, min(r, p.n_pos - 1));
+                    const float* c = p.rope + r * p.rot + item * E;
+                    rotate_halves<T>(lo2[t], hi2[t], c, c + p.rot / 2);
+                    *(vec*)(out + (int64_t)t * p.n_q * (D * (int)sizeof(T))) = lo2[t];
+                    *(vec*)(out + (int64_t)t * p.n_q * (D * (int)sizeof(T)) + far) = hi2[t];
+                }
+                continue;
+            }
+            for (int token = t0 + x; token < t1; token += side) {
+                if (p.b.q_start)
+                    while (q + 1 < p.b.n_seq && p.b.q_start[q + 1] <= token) kv_seq(p.b, ++q, first, n, len);
+                else if (q != token)
+                    kv_seq(p.b, q = token, first, n, len);
+                if (token < first || token >= first + n) continue;
+                char* out = p.q_out + ((int64_t)token * p.n_q + head) * (D * (int)sizeof(T));
+                row_item<T, D>(p, p.q + token * p.q_ts + head * p.q_hs, item, token, len - n + (token - first),
+                               [&](int g, vec z) { *(vec*)(out + g * 16) = z; });
+            }
+        }
         return;
     }
 
     // one page of one head
+    __shared__ __align__(16) char lk[SLAB * ROW], lv[SLAB * ROW];
     const int h = blockIdx.x % p.n_kv;
     const int logp = p.b.log_page, P = 1 << logp;
-    int s, j;
-    auto count = [&](int q) {
-        int first, n, len;
-        kv_seq(p.b, q, first, n, len);
-        const int p0 = max(0, len - n);
-        return n > 0 && len > 0 ? ((len - 1) >> logp) - (p0 >> logp) + 1 : 0;
-    };
-    if (!kv_find(p.b.n_seq, blockIdx.x / p.n_kv, count, s, j)) return;
-    int first, n, len;
-    kv_seq(p.b, s, first, n, len);
+    int s, j, first, n, len;
+    auto count = [&](int n, int len) { return n > 0 && len > 0 ? ((len - 1) >> logp) - (max(0, len - n) >> logp) + 1 : 0; };
+    if (!kv_find(p.b, blockIdx.x / p.n_kv, count, s, j, first, n, len)) return;
     const int p0 = len - n;                          // position of the first new token (negative: tokens before the sequence)
     const int blk = (max(0, p0) >> logp) + j;
     const int page = kv_page(p.b, s, blk);
@@ -124,57 +154,117 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs p) {
     const int64_t at = ((int64_t)page * p.n_kv + h) * ((int64_t)P * D * (int)sizeof(T));
     char* kp = p.kc + at;
     char* vp = p.vc + at;
-    for (int i = tid; i < (hi - lo) * items; i += kThreads) {
-        const int slot = lo + i / items, token = first + (base + slot - p0);
-        row_item<T, D>(p, p.k + token * p.k_ts + h * p.k_hs, i % items, token, base + slot,
-                       [&](int g, vec x) { *(vec*)(kp + ((int64_t)g * P + slot) * 16) = x; });
-    }
-    for (int i = tid; i < ((hi + E - 1) / E - lo / E) * D; i += kThreads) {      // E slots of one channel
-        const int c = i % D, g = lo / E + i / D;
-        const char* src = p.v + h * p.v_hs + c * (int)sizeof(T);
-        vec x;
+    // this thread's channels and remainder of the slots in the signature's sums
+    constexpr int PAIR = E == 8 ? 2 : 1, SUMS = D / PAIR * 8 / kThreads;
+    float sum[SUMS][PAIR] = {};
+    for (int s0 = p.sig ? 0 : lo & ~(SLAB - 1); s0 < hi; s0 += SLAB) {
+        const int a = max(lo - s0, 0), b = min(hi - s0, SLAB);       // new ones of the slab: a .. b - 1; before them older ones
+        if (p.sig)
+            for (int i = tid; i < min(a, b) * NG; i += kThreads) {
+                const int g = i / min(a, b), slot = i % min(a, b);
+                *(vec*)(lk + slot * ROW + g * 16) = *(const vec*)(kp + ((int64_t)g * P + s0 + slot) * 16);
+            }
+        const char* vrow = p.v + h * p.v_hs;
+        const char* krow = p.k + h * p.k_hs;
+        const int t0 = first + (base + s0 - p0);                     // the slab's first slot, were it new
+        if (b - a == SLAB && !p.inter) {
+            // a whole slab: a thread has one group of channels in every IT-th slot, and takes its partners' channels from the same rows
+            constexpr int STEP = kThreads / NG, IT = SLAB / STEP;
+            const int g = tid % NG, slot = tid / NG, halves = p.rope ? p.rot / (2 * E) : 0;
+            const bool up = g < halves, turned = g < 2 * halves;
+            const int mate = up ? g + halves : turned ? g - halves : g;
+            vec v[IT];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int slot = g * E + e;
-            if (slot >= lo && slot < hi) x[e] = *(const T*)(src + (int64_t)(first + (base + slot - p0)) * p.v_ts);
-        }
-        vec* dst = (vec*)(vp + ((int64_t)g * D + c) * 16);
-        if (g * E >= lo && g * E + E <= hi) {
-            *dst = x;
+            for (int x = 0; x < IT; ++x) v[x] = *(const vec*)(vrow + (int64_t)(t0 + slot + x * STEP) * p.v_ts + g * 16);
+#pragma unroll 2
+            for (int x = 0; x < IT; ++x) {
+                const int token = t0 + slot + x * STEP;
+                const char* row = krow + (int64_t)token * p.k_ts;
+                vec own = *(const vec*)(row + g * 16);
+                if (turned) {
+                    const vec other = *(const vec*)(row + mate * 16);
+                    int64_t r = p.positions ? p.positions[token] : base + s0 + slot + x * STEP;
+                    r = max((int64_t)0, min(r, p.n_pos - 1));
+                    const float* c = p.rope + r * p.rot + min(g, mate) * E;
+                    vec lo2 = up ? own : other, hi2 = up ? other : own;
+                    rotate_halves<T>(lo2, hi2, c, c + p.rot / 2);
+                    own = up ? lo2 : hi2;
+                }
+                *(vec*)(lk + (slot + x * STEP) * ROW + g * 16) = own;
+            }
+#pragma unroll
+            for (int x = 0; x < IT; ++x) *(vec*)(lv + (slot + x * STEP) * ROW + g * 16) = v[x];
         } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (g * E + e >= lo && g * E + e < hi) ((T*)dst)[e] = x[e];
+            for (int i = tid; i < (b - a) * NG; i += kThreads) {
+                const int slot = a + i / NG, g = i % NG;
+                *(vec*)(lv + slot * ROW + g * 16) = *(const vec*)(vrow + (int64_t)(t0 + slot) * p.v_ts + g * 16);
+            }
+            for (int i = tid; i < (b - a) * items; i += kThreads) {
+                const int slot = a + i / items;
+                row_item<T, D>(p, krow + (int64_t)(t0 + slot) * p.k_ts, i % items, t0 + slot, base + s0 + slot,
+                               [&](int g, vec x) { *(vec*)(lk + slot * ROW + g * 16) = x; });
+            }
         }
+        __syncthreads();
+        if (b - a == SLAB) {
+            for (int i = tid; i < SLAB * NG; i += kThreads) {
+                const int g = i / SLAB, slot = i % SLAB;
+                *(vec*)(kp + ((int64_t)g * P + s0 + slot) * 16) = *(const vec*)(lk + slot * ROW + g * 16);
+            }
+        } else {
+            for (int i = tid; i < (b - a) * NG; i += kThreads) {
+                const int g = i / (b - a), slot = a + i % (b - a);
+                *(vec*)(kp + ((int64_t)g * P + s0 + slot) * 16) = *(const vec*)(lk + slot * ROW + g * 16);
+            }
+        }
+        for (int i = tid; b > a && i < ((b + E - 1) / E - a / E) * D; i += kThreads) {      // E slots of one channel
+            const int c = i % D, g = a / E + i / D;
+            vec x;
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = *(const T*)(lv + (g * E + e) * ROW + c * (int)sizeof(T));      // of other slots: not stored
+            vec* dst = (vec*)(vp + ((int64_t)(s0 / E + g) * D + c) * 16);
+            if (g * E >= a && g * E + E <= b) {
+                *dst = x;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (g * E + e >= a && g * E + e < b) ((T*)dst)[e] = x[e];
+            }
+        }
+        if (p.sig) {
+#pragma unroll
+            for (int y = 0; y < SUMS; ++y) {
+                const int i = tid + y * kThreads, r = i / (D / PAIR), c = i % (D / PAIR) * PAIR;
+                for (int slot = r; slot < b; slot += 8) {
+#pragma unroll
+                    for (int e = 0; e < PAIR; ++e) sum[y][e] += (float)*(const T*)(lk + slot * ROW + (c + e) * (int)sizeof(T));
+                }
+            }
+        }
+        __syncthreads();
     }
     if (!p.sig) return;
-    __shared__ float part[8][D];
-    __shared__ unsigned biggest;
-    if (tid == 0) biggest = 0;
-    __threadfence_block();
-    __syncthreads();
-    for (int i = tid; i < NG * 8; i += kThreads) {
-        const int g = i >> 3, r = i & 7;
-        float sum[E] = {};
-        for (int slot = r; slot < hi; slot += 8) {
-            const vec x = *(const vec*)(kp + ((int64_t)g * P + slot) * 16);
+    __shared__ unsigned biggest[kThreads / 64];
+    float* part = (float*)lk;                        // [8][D]
+    static_assert(sizeof(lk) >= 8 * D * sizeof(float), "sums fit the slab");
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[e] += (float)x[e];
-        }
+    for (int y = 0; y < SUMS; ++y)
 #pragma unroll
-        for (int e = 0; e < E; ++e) part[r][g * E + e] = sum[e];
-    }
+        for (int e = 0; e < PAIR; ++e) part[(tid + y * kThreads) * PAIR + e] = sum[y][e];
     __syncthreads();
     float m = 0.0f;
-    if (tid < D) {
-        m = (((part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid])) +
-             ((part[4][tid] + part[5][tid]) + (part[6][tid] + part[7][tid]))) / (float)hi;
-        atomicMax(&biggest, __float_as_uint(m) & 0x7fffffffu);
-    }
+    if (tid < D)
+        m = (((part[tid] + part[D + tid]) + (part[2 * D + tid] + part[3 * D + tid])) +
+             ((part[4 * D + tid] + part[5 * D + tid]) + (part[6 * D + tid] + part[7 * D + tid]))) / (float)hi;
+    const unsigned big = s3_wave_max_u32(__float_as_uint(m) & 0x7fffffffu);
+    if ((tid & 63) == 0) biggest[tid >> 6] = big;
     __syncthreads();
     if (tid < D) {
+        unsigned most = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 64; ++w) most = max(most, biggest[w]);
         bool ok;
-        const int e = kv_grid_exp(biggest, ok);
+        const int e = kv_grid_exp(most, ok);
         p.sig[((int64_t)page * p.n_kv + h) * D + tid] = (__bf16)(ok ? kv_grid(m, e) : 0.0f);
     }
 }
@@ -193,9 +283,7 @@ __global__ void kv_rope_kernel(float* table, int64_t n_pos, int half, double log
 template <typename T, int D>
 int launch_append(const AppendArgs& p, hipStream_t st) {
     AppendArgs a = p;
-    const int E = KvElem<T>::E;
-    const int64_t items = a.rope && !a.inter ? D / E - a.rot / (2 * E) : D / E;
-    const int64_t qb = a.q ? ((int64_t)a.b.n_tokens * a.n_q * items + kThreads - 1) / kThreads : 0;
+    const int64_t qb = a.q ? (a.b.n_tokens + a.group - 1) / a.group : 0;
     const int64_t grid = (int64_t)a.page_items + qb;
     if (grid >= (int64_t)1 << 24) return s3_fail(S3_EINVAL, "s3_kv_append: too many tokens in one call");
     hipLaunchKernelGGL((kv_append_kernel<T, D>), dim3((unsigned)grid), dim3(kThreads), 0, st, a);
@@ -266,7 +354,7 @@ extern "C" int s3_kv_append(const s3_kv_cache* c, const s3_kv_batch* b, const vo
     if (pages * c->n_kv_heads >= (int64_t)1 << 24) return s3_fail(S3_EINVAL, "%s: too many tokens in one call", fn);
     AppendArgs p{s3_kv_batch_args(c, b), (char*)c->k, (char*)c->v, (__bf16*)c->sig, (const char*)k, (const char*)v, (const char*)q,
                  (char*)q_out, k_ts * es, k_hs * es, v_ts * es, v_hs * es, q_ts * es, q_hs * es, rope, positions, n_pos, rot_dim,
-                 interleaved != 0, c->n_kv_heads, n_q, (unsigned)(pages * c->n_kv_heads)};
+                 interleaved != 0, c->n_kv_heads, n_q, (unsigned)(pages * c->n_kv_heads), b->n_tokens >= 512 ? kTokens : 1};
     hipStream_t st = (hipStream_t)stream;
     if (c->dtype == S3_BF16) {
         if (c->d_head == 64) return launch_append<__bf16, 64>(p, st);

@@ -53,22 +53,28 @@ __device__ __forceinline__ int kv_page(const KvBatch& b, int s, int blk) {
     return p >= 0 && p < b.n_pages ? p : -1;
 }
 
-// Item `item` of a list in which sequence s has count(s) entries: which sequence, and which of its entries.  Run by a whole
-// wavefront; false where the list is shorter.
+// Item `item` of a list in which a sequence has count(n, len) entries: which sequence (and kv_seq's values of it), and which of its
+// entries.  Run by a whole wavefront, 64 sequences at a time; false where the list is shorter.
 template <typename F>
-__device__ __forceinline__ bool kv_find(int n_seq, int64_t item, F count, int& seq, int& local) {
+__device__ __forceinline__ bool kv_find(const KvBatch& b, int64_t item, F count, int& seq, int& local, int& first, int& n, int& len) {
     const int lane = threadIdx.x & 63;
     int64_t run = 0;
-    for (int base = 0; base < n_seq; base += 64) {
-        const int s = base + lane;
-        const int c = s < n_seq ? count(s) : 0;
+    for (int base = 0; base < b.n_seq; base += 64) {
+        int f = 0, m = 0, l = 0, c = 0;
+        if (base + lane < b.n_seq) {
+            kv_seq(b, base + lane, f, m, l);
+            c = count(m, l);
+        }
         const int incl = s3_wave_incl_scan(c);
         const int total = __builtin_amdgcn_readlane(incl, 63);
         if (item < run + total) {
             const int want = (int)(item - run);
-            const int l = __builtin_ctzll(__ballot(incl > want));
-            seq = base + l;
-            local = want - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l));
+            const int x = __builtin_ctzll(__ballot(incl > want));
+            seq = base + x;
+            local = want - (__builtin_amdgcn_readlane(incl, x) - __builtin_amdgcn_readlane(c, x));
+            first = __builtin_amdgcn_readlane(f, x);
+            n = __builtin_amdgcn_readlane(m, x);
+            len = __builtin_amdgcn_readlane(l, x);
             return true;
         }
         run += total;

@@ -32,13 +32,7 @@ struct Tile {
     int s, first, n, len, t0, t1, nb;      // tokens t0 .. t1 - 1 of the sequence's n; candidates 0 .. nb - 1
     __device__ __forceinline__ bool find(const SelectArgs& p, int tile) {
         int j;
-        auto count = [&](int q) {
-            int f, m, l;
-            kv_seq(p.b, q, f, m, l);
-            return (m + p.qb - 1) / p.qb;
-        };
-        if (!kv_find(p.b.n_seq, tile, count, s, j)) return false;
-        kv_seq(p.b, s, first, n, len);
+        if (!kv_find(p.b, tile, [&](int m, int) { return (m + p.qb - 1) / p.qb; }, s, j, first, n, len)) return false;
         t0 = j * p.qb;
         t1 = min(n, t0 + p.qb);
         const int last = len - n + t1 - 1;
