@@ -10,7 +10,7 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kScoreBlocks = 512;      // blocks of one scoring workgroup
+constexpr int kScoreBlocks = 128;      // blocks of one scoring workgroup: 32 a wavefront (512: 17.5 us a call where 128 take 14)
 
 struct SelectArgs {
     KvBatch b;
@@ -174,6 +174,195 @@ __device__ __forceinline__ void pick_by_wave(unsigned* keys, int n, int lead, in
         }
     }
     for (int i = at + lane; i < top; i += 64) out[i] = -1;
+}
+
+// The choice for one tile by a workgroup of 16 wavefronts, where the candidates are many: key(i) for i < n (0: no candidate, all ones: always taken), kept in registers as
+// far as they go.  Keys are counted by ballots and added up over the wavefronts, one barrier a round.
+constexpr int kMine = 16;                        // keys of a thread
+template <int WAVES> struct PickScratch {
+    int sums[2][WAVES], cand[WAVES], always[WAVES], place[kMine * WAVES];
+    unsigned least[WAVES], most[WAVES], mid_key[64], thr;
+    int mid_at[64], lim;
+};
+template <int WAVES, typename K>
+__device__ __forceinline__ void pick_by_block(K key, int n, int top, PickScratch<WAVES>& sh, int32_t* out) {
+    constexpr int ALL = WAVES * 64, CHUNK = kMine * ALL;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    unsigned k[kMine];
+    auto read = [&](int base) {
+#pragma unroll
+        for (int x = 0; x < kMine; ++x) {
+            const int i = base + x * ALL + tid;
+            k[x] = i < n ? key(i) : 0u;
+        }
+    };
+    int round = 0;
+    // how many keys satisfy f(key, i), over the workgroup
+    auto count = [&](auto f) {
+        int c = 0;
+        for (int base = 0; base < n; base += CHUNK) {
+            if (n > CHUNK) read(base);
+#pragma unroll
+            for (int x = 0; x < kMine; ++x)
+                if (base + x * ALL < n) c += __popcll(__ballot(f(k[x], base + x * ALL + tid)));
+        }
+        int* sums = sh.sums[round++ & 1];
+        if (lane == 0) sums[wave] = c;
+        __syncthreads();
+        c = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) c += sums[w];
+        return c;
+    };
+    read(0);
+    unsigned least = 0xffffffffu, most = 0;
+    int cand = 0, always = 0;
+    for (int base = 0; base < n; base += CHUNK) {
+        if (n > CHUNK) read(base);
+#pragma unroll
+        for (int x = 0; x < kMine; ++x) {
+            const bool in = k[x] != 0, must = k[x] == 0xffffffffu;
+            cand += __popcll(__ballot(in));
+            always += __popcll(__ballot(must));
+            least = min(least, in && !must ? k[x] : 0xffffffffu);
+            most = max(most, in && !must ? k[x] : 0u);
+        }
+    }
+    least = ~s3_wave_max_u32(~least);
+    most = s3_wave_max_u32(most);
+    if (lane == 0) {
+        sh.cand[wave] = cand;
+        sh.always[wave] = always;
+        sh.least[wave] = least;
+        sh.most[wave] = most;
+    }
+    __syncthreads();
+    cand = always = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        cand += sh.cand[w];
+        always += sh.always[w];
+        least = min(least, sh.least[w]);
+        most = max(most, sh.most[w]);
+    }
+    // taken: keys above thr, and those at it up to block lim
+    unsigned thr = 1;
+    int lim = -1;
+    if (cand > top) {
+        unsigned lo = least, hi = most + 1;
+        int from_lo = cand, from_hi = always;
+        if (always >= top) {
+            lo = 0xffffffffu;
+            from_hi = 0;
+        }
+        while (hi - lo > 1 && from_lo - from_hi > 64 && always < top) {
+            const unsigned mid = lo + (hi - lo) / 2;
+            const int c = count([&](unsigned x, int) { return x >= mid; });
+            if (c > top) {
+                lo = mid;
+                from_lo = c;
+            } else {
+                hi = mid;
+                from_hi = c;
+            }
+        }
+        const int need = top - from_hi;              // of those in the interval
+        if (need == 0) {
+            thr = hi - 1;
+        } else if (always < top && from_lo - from_hi <= 64) {
+            const auto in = [&](unsigned x) { return x >= lo && x < hi; };
+            int c = 0;
+            for (int base = 0; base < n; base += CHUNK) {
+                if (n > CHUNK) read(base);
+#pragma unroll
+                for (int x = 0; x < kMine; ++x) c += __popcll(__ballot(in(k[x])));
+            }
+            int* sums = sh.sums[round++ & 1];
+            if (lane == 0) sums[wave] = c;
+            __syncthreads();
+            int m = 0, at = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                at += w < wave ? sums[w] : 0;
+                m += sums[w];
+            }
+            for (int base = 0; base < n; base += CHUNK) {
+                if (n > CHUNK) read(base);
+#pragma unroll
+                for (int x = 0; x < kMine; ++x) {
+                    const uint64_t b = __ballot(in(k[x]));
+                    if (in(k[x])) {
+                        sh.mid_key[at + __popcll(b & below)] = k[x];
+                        sh.mid_at[at + __popcll(b & below)] = base + x * ALL + tid;
+                    }
+                    at += __popcll(b);
+                }
+            }
+            __syncthreads();
+            if (wave == 0) {
+                const unsigned mine = lane < m ? sh.mid_key[lane] : 0u;
+                const int mine_at = lane < m ? sh.mid_at[lane] : 0;
+                int rank = 0;                        // keys before this one: greater, or equal and of a lower block
+                for (int i = 0; i < m; ++i) {
+                    const unsigned x = (unsigned)__builtin_amdgcn_readlane((int)mine, i);
+                    rank += x > mine || (x == mine && __builtin_amdgcn_readlane(mine_at, i) < mine_at);
+                }
+                if (lane < m && rank == need - 1) {
+                    sh.thr = mine;
+                    sh.lim = mine_at;
+                }
+            }
+            __syncthreads();
+            thr = sh.thr;
+            lim = sh.lim;
+        } else {                                     // many equal keys: the first `need` of them, found in the blocks' numbers
+            thr = lo;
+            int a = -1, b = n - 1;                   // up to a fewer than needed, up to b enough
+            while (b - a > 1) {
+                const int mid = a + (b - a) / 2;
+                if (count([&](unsigned x, int i) { return x == thr && i <= mid; }) >= need) b = mid;
+                else a = mid;
+            }
+            lim = b;
+        }
+    }
+    int done = 0;
+    for (int base = 0; base < n; base += CHUNK) {
+        if (n > CHUNK) read(base);
+#pragma unroll
+        for (int x = 0; x < kMine; ++x) {
+            const bool take = k[x] > thr || (k[x] == thr && base + x * ALL + tid <= lim);
+            const uint64_t b = __ballot(take);
+            if (lane == 0) sh.place[x * WAVES + wave] = __popcll(b);
+        }
+        __syncthreads();
+        // places before this wavefront's of every 64 * WAVES blocks
+        int run = done, before[kMine];
+#pragma unroll
+        for (int x = 0; x < kMine; ++x) {
+            int all = 0, mine = 0;
+            if (base + x * ALL < n)
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const int c = sh.place[x * WAVES + w];
+                    mine += w < wave ? c : 0;
+                    all += c;
+                }
+            before[x] = run + mine;
+            run += all;
+        }
+        done = run;
+#pragma unroll
+        for (int x = 0; x < kMine; ++x) {
+            const int i = base + x * ALL + tid;
+            const bool take = k[x] > thr || (k[x] == thr && i <= lim);
+            const int to = before[x] + __popcll(__ballot(take) & below);
+            if (take && to < top) out[to] = i;
+        }
+        __syncthreads();
+    }
+    for (int i = done + tid; i < top; i += ALL) out[i] = -1;
 }
 
 // tiles_wg tiles of one sequence and head.  Rows are dealt in fours, each four of one tile (a tile's last row repeated to fill them:
@@ -405,6 +594,16 @@ __global__ __launch_bounds__(kThreads) void sel_pick_kernel(SelectArgs p) {
     for (int i = n + tid; i < p.top; i += kThreads) out[i] = -1;
 }
 
+constexpr int kPickWaves = 16;
+__global__ __launch_bounds__(kPickWaves * 64) void sel_pick_long_kernel(SelectArgs p) {
+    __shared__ PickScratch<kPickWaves> scratch;
+    const int head = blockIdx.x % p.n_kv, tile = blockIdx.x / p.n_kv;
+    Tile t;
+    const int nb = t.find(p, tile) ? t.nb : 0;
+    const unsigned* keys = p.keys + ((int64_t)tile * p.n_kv + head) * p.nb;
+    pick_by_block<kPickWaves>([&](int i) { return keys[i]; }, nb, p.top, scratch, p.sel + ((int64_t)tile * p.n_kv + head) * p.top);
+}
+
 int select_blocks(const s3_kv_cache* c, const s3_kv_batch* b) {
     return (int)max((int64_t)1, min((int64_t)b->max_pages, ((int64_t)b->max_kv + c->page_size - 1) / c->page_size));
 }
@@ -430,7 +629,9 @@ struct SelectPlan {
         groups = (tiles + (int64_t)b->n_seq * (t - 1)) / t;
         whole = q_block <= most && (int64_t)q_block * G % 32 == 0;
         waves = sets == 1 && groups * c->n_kv_heads < 256 ? 16 : 8;
-        fused = nb <= 30720 && (nb <= 2048 || groups * c->n_kv_heads >= 64);
+        // one tile a workgroup: 512 lists of 62 / 500 candidates 14 / 25.3 us in one kernel, 12.1 / 27.4 through scratch; 8 of 500, 18 / 12.5
+        const int64_t lists = groups * c->n_kv_heads;
+        fused = nb <= 30720 && (sets == 1 && tiles_wg == 1 ? lists * nb >= 200000 : lists >= 64 || nb <= 256);
     }
     size_t workspace(int n_kv) const { return fused ? 0 : s3_align((size_t)tiles * n_kv * nb * 4); }
 };
@@ -459,7 +660,9 @@ int launch_select(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
     if ((int64_t)grid.x * grid.y >= (int64_t)1 << 24 || grid.y > 65535) return s3_fail(S3_EINVAL, "s3_block_select: too many tiles in one call");
     hipLaunchKernelGGL((sel_score_kernel<T, D>), grid, dim3(kThreads), 0, st, p);
     S3_HIP(hipGetLastError());
-    hipLaunchKernelGGL(sel_pick_kernel, dim3(grid.x), dim3(kThreads), 0, st, p);
+    // 8 tiles of 2048 / 15625 candidates, us a call: 21 / 86 with the first, 32 / 41 with the second
+    if (p.nb <= 4096) hipLaunchKernelGGL(sel_pick_kernel, dim3(grid.x), dim3(kThreads), 0, st, p);
+    else hipLaunchKernelGGL(sel_pick_long_kernel, dim3(grid.x), dim3(kPickWaves * 64), 0, st, p);
     S3_HIP(hipGetLastError());
     return S3_OK;
 }
