@@ -415,7 +415,8 @@ int s3_paged_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const
  * (whole multiples of one power of two: exact in fp32 in any order, so the choice is the same everywhere).  Candidates are
  * the mapped blocks up to that of the tile's last position.  The first `lead` of them, and with tail > 0 those from
  * tail - 1 before the block of the tile's first position on, are always taken; then the largest scores, ties to the lower block.
- *   sel [s3_block_tiles(batch, q_block)][n_kv_heads][top_b] int32: the chosen blocks in ascending order, then -1.
+ *   sel [s3_block_tiles(batch, q_block)][n_kv_heads][top_b] int32: the chosen blocks in ascending order, then -1 (tiles beyond the
+ *       last one of the batch: all -1; s3_block_tiles is what n_tokens and n_seq allow).
  *   ws  s3_block_select_workspace(...) bytes, 256-byte aligned.
  * Limits: cache->sig; q_block >= 1; 1 <= top_b <= 4096; lead, tail >= 0; lead + tail + (q_block + page_size - 2) / page_size <= top_b. */
 int64_t s3_block_tiles(const s3_kv_batch* batch, int q_block);

@@ -22,6 +22,10 @@ SHAPES = [   # dtype, d, P, hq, hkv, new, kv
     ("fp32", 256, 32, 4, 2, [1, 40], [100, 65]),
     ("bf16", 256, 64, 4, 2, [150], [150]),                            # a whole prompt
     ("bf16", 128, 32, 4, 1, [300], [301]),
+    ("bf16", 128, 64, 4, 1, [70], [9000]),                            # the tokens of a row tile in parts
+    ("fp32", 64, 64, 4, 2, [200, 3], [700, 2000]),
+    ("fp32", 128, 32, 4, 2, [90], [1500]),
+    ("bf16", 64, 64, 32, 1, [3, 1], [900, 40]),                       # 96 rows of three tokens
 ]
 
 
@@ -321,6 +325,55 @@ def test_select_ties_and_unmapped_blocks():
     sel = pr.cache(sig=sig).select(pr.q.cuda(), kv_len, table, 7, q_start=pr.q_start.cuda(), q_block=1)
     assert np.array_equal(sel.cpu().numpy(), paged.select(pr, sig, 7, 1, 1, 1))
     assert sel[2, 0].tolist() == [1, 2, 3, 5, 6, 7, 49]
+
+
+@pytest.mark.parametrize("n_blocks,new,qb,top,kinds", [
+    (300, 1, 1, 40, 0), (300, 1, 1, 40, 3),                           # through scratch; three different signatures only: ties everywhere
+    (2000, 40, 8, 200, 0), (2000, 40, 8, 200, 5),
+    (5000, 1, 1, 64, 0), (5000, 1, 1, 64, 2),                         # the pick of many candidates
+    (20000, 3, 1, 700, 0), (20000, 3, 1, 700, 40),                    # more than it keeps in registers
+    (20000, 1, 1, 4096, 0),
+    (700, 130, 1, 30, 0), (700, 130, 1, 30, 2),                       # several tiles a workgroup
+])
+def test_select_of_many_candidates(n_blocks, new, qb, top, kinds):
+    import paper_2601_17702_amd as s3
+    kv = n_blocks * 16 - 3
+    pr = paged.Problem(n_blocks + new, "bf16", 64, 16, 4, 2, [new], [kv])
+    sig = draw_sig(pr)
+    if kinds:
+        sig = sig[torch.randint(0, kinds, (pr.n_pages,), generator=pr.g)]
+    pr.table[0, 7] = -1
+    c = s3.KVCache(pr.n_pages, 16, 2, 64, sig=sig.cuda())
+    kv_len, table = pr.args()
+    sel = c.select(pr.q.cuda(), kv_len, table, top, q_start=pr.q_start.cuda(), q_block=qb, lead=2, tail=2, max_new=new, max_kv=kv)
+    assert np.array_equal(sel.cpu().numpy(), paged.select(pr, sig, top, qb, 2, 2))
+
+
+@pytest.mark.parametrize("new,G,n_seq,listed", [(1, 4, 1200, False), (1, 4, 1200, True), (64, 4, 300, False), (64, 4, 300, True)])
+def test_many_sequences_over_the_same_pages(new, G, n_seq, listed):
+    """A shared prefix, and more work a workgroup than it looks up pages for at a time: every sequence has the same answer."""
+    kv, P = 20000, 64
+    pr = paged.Problem(n_seq + new, "bf16", 64, P, G, 1, [new], [kv])
+    n_blocks = -(-kv // P)
+    sel = np.arange(n_blocks, dtype=np.int32).reshape(1, 1, n_blocks) if listed else None
+    want = paged.attend(pr, sel=sel, qb=new if listed else None)
+    q = pr.q.cuda().repeat(n_seq, 1, 1)
+    kv_len = torch.full((n_seq,), kv, dtype=torch.int32, device="cuda")
+    table = pr.table.cuda().repeat(n_seq, 1)
+    qs = torch.arange(n_seq + 1, dtype=torch.int32, device="cuda") * new
+    c = pr.cache()
+    if listed:
+        tiles = (n_seq * new + n_seq * (new - 1)) // new               # the list's documented length; one tile a sequence is used
+        dev = torch.from_numpy(sel).cuda().repeat(tiles, 1, 1)
+        o, lse = c.block_attention(q, kv_len, table, dev, q_start=qs, q_block=new, want_lse=True)
+    else:
+        o, lse = c.attention(q, kv_len, table, q_start=qs, max_new=new, max_kv=kv, want_lse=True)
+    o, lse = o.view(n_seq, new, G, 64), lse.view(n_seq, new, G)
+    paged.check(pr, o[0], lse[0], want)
+    tol = want[2].cuda().to(torch.float32) * 2
+    assert torch.all((o.float() - o[:1].float()).abs() <= tol)         # where a workgroup's run ends differs, so do roundings
+    for s in (1, n_seq // 2, n_seq - 1):
+        paged.check(pr, o[s], lse[s], want)
 
 
 @pytest.mark.parametrize("dtype,d,P,hq,hkv,new,kv,qb,top", [
