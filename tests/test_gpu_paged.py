@@ -451,6 +451,24 @@ def test_captured_in_a_graph(new):
             assert torch.equal(a, b)
 
 
+# ------------------------------------------------------------------------------------------------ all of it together
+def test_example_of_a_context_answered_from_a_part_of_it():
+    """examples/paged_answer.py: lists hold blocks of the cache in ascending order, the named ones those of the spans; a part of
+    the blocks cannot hold more than all of the weight, and holds more than its share of the cache where keys and question share a topic."""
+    from examples import paged_answer
+    r = paged_answer.run(context=3000, chunk=700, answer=3, n_q=8, n_kv=2, n_feat=1024, k=16, top_blocks=12, n_spans=6)
+    assert torch.isfinite(r["hidden"].float()).all() and torch.isfinite(r["full"].float()).all()
+    for sel in (r["named"], r["chosen"]):
+        for row in sel.cpu().view(-1, 12).tolist():
+            there = [b for b in row if b >= 0]
+            assert there == sorted(set(there)) and there[0] == 0 and there[-1] == r["blocks"] - 1 and row[len(there):] == [-1] * (12 - len(there))
+    named = set(r["named"].cpu().view(-1).tolist())
+    spans = [int(s) for s in r["starts"].cpu() if s >= 0]
+    assert spans and sum(s // 64 in named for s in spans) >= min(len(spans), 4)
+    share = 12 / r["blocks"]
+    assert share < r["chosen_share"] <= 1.0 + 1e-5 and 0.0 < r["span_share"] <= 1.0 + 1e-5
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 def test_refusals():
     import paper_2601_17702_amd as s3
