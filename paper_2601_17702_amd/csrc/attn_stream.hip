@@ -1,17 +1,19 @@
-// Attention of few rows: sequences (or tiles of listed blocks) whose new tokens times query heads per key/value head are 32 at most.
+// Attention of few rows: sequences (or tiles of listed blocks) whose new tokens times query heads per key/value head are 128 at most.
 //
-// The work is one pass over the keys and values, so memory bounds it: 64 decoding steps of 300 to 32768 tokens (1.85 GB)
-// take 373 us, 5.0 TB/s (a copy moves 4.8).  All of it, over all sequences and heads, is one line of pieces of 128 tokens, and every
+// The work is one pass over the keys and values, so memory bounds it: 64 decoding steps of 300 to 32768 tokens (1.86 GB)
+// take 350 us, 5.3 TB/s (a copy moves 4.8).  All of it, over all sequences and heads, is one line of pieces of 128 tokens, and every
 // workgroup takes an equal run of that line whatever the lengths are: a long sequence is shared by many workgroups, short ones lie
 // whole in one.  A workgroup's four wavefronts take 32 tokens of a piece each, keys and values straight from memory into the
-// matrix instructions' operands (nobody else in the workgroup wants them), the next 32 tokens' keys on their way while the
-// weights are made and the next values during the next scores.  Where a run ends inside a row tile, its sums go to scratch,
-// and a second kernel joins them.
+// matrix instructions' operands, the next 32 tokens' keys on their way while the weights are made and the next values
+// during the next scores.  Where a run ends inside a row tile, its sums go to scratch, and a second kernel joins them.
+// Of 64 or 128 rows, RT sets of 32, the wavefronts have a set each and a piece has as many fewer tokens: those with the same tokens find them
+// in the compute unit's cache (4300 MB of listed blocks of a long cache: 758 us where each set read its own, 419 so).
 #include "attn_launch.h"
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kPiece = 32 * kWaves;
+constexpr int kThreads = 256, kWaves = 4;
+template <int RT> constexpr int kPiece = 32 * kWaves / RT;      // tokens of a piece: 32 for every wavefront of a row set
 constexpr int kRunGroups = 512;        // workgroups that share the line: two per compute unit
 constexpr int kBatchRuns = 1024;       // runs of 16 tokens whose pages are looked up at a time
 
@@ -28,45 +30,45 @@ __device__ __forceinline__ int64_t wave_incl_scan64(int64_t x) {
 struct Part {
     int first, n, len, lo, tiles, pieces;
 };
-template <bool LIST>
+template <bool LIST, int RT>
 __device__ __forceinline__ Part part_of(const AttnArgs& p, int s) {
     Part r;
     kv_seq(p.b, s, r.first, r.n, r.len);
     r.lo = 0;
     if (LIST) {
         r.tiles = (r.n + p.qb - 1) / p.qb * p.per_q;
-        r.pieces = ((p.top << p.b.log_page) + kPiece - 1) / kPiece;
+        r.pieces = ((p.top << p.b.log_page) + kPiece<RT> - 1) / kPiece<RT>;
     } else {
-        r.tiles = r.n * p.G <= p.few ? (r.n * p.G + 31) / 32 : 0;
+        r.tiles = r.n * p.G <= p.few ? (r.n * p.G + 32 * RT - 1) / (32 * RT) : 0;
         if (p.window) r.lo = max(0, r.len - r.n - p.window + 1) & ~31;
         const int hi = min(r.len, kv_blocks(p.b, r.len) << p.b.log_page);
-        r.pieces = (max(hi - r.lo, 1) + kPiece - 1) / kPiece;         // one at least: rows that see nothing are written, too
+        r.pieces = (max(hi - r.lo, 1) + kPiece<RT> - 1) / kPiece<RT>;         // one at least: rows that see nothing are written, too
     }
     return r;
 }
 
 // Rows of a tile: the first, and the end.
-template <bool LIST>
+template <bool LIST, int RT>
 __device__ __forceinline__ void rows_of(const AttnArgs& p, const Part& part, int tile, int& r0, int& r_end) {
     if (LIST) {
         const int qt = tile / p.per_q;
-        r0 = qt * p.qb * p.G + (tile - qt * p.per_q) * 32;
-        r_end = min(min(part.n, (qt + 1) * p.qb) * p.G, r0 + 32);
+        r0 = qt * p.qb * p.G + (tile - qt * p.per_q) * (32 * RT);
+        r_end = min(min(part.n, (qt + 1) * p.qb) * p.G, r0 + 32 * RT);
     } else {
-        r0 = tile * 32;
-        r_end = min(part.n * p.G, r0 + 32);
+        r0 = tile * (32 * RT);
+        r_end = min(part.n * p.G, r0 + 32 * RT);
     }
 }
 
 // The line's length and equal runs of it.
-template <bool LIST>
+template <bool LIST, int RT>
 __device__ __forceinline__ int64_t line_length(const AttnArgs& p) {
     int64_t total = 0;
     for (int base = 0; base < p.b.n_seq; base += 64) {
         const int s = base + (threadIdx.x & 63);
         int64_t c = 0;
         if (s < p.b.n_seq) {
-            const Part r = part_of<LIST>(p, s);
+            const Part r = part_of<LIST, RT>(p, s);
             c = (int64_t)r.tiles * r.pieces * p.n_kv;
         }
         total += __shfl(wave_incl_scan64(c), 63);
@@ -74,9 +76,9 @@ __device__ __forceinline__ int64_t line_length(const AttnArgs& p) {
     return total;
 }
 
-template <typename T, int D, bool LIST>
+template <typename T, int D, bool LIST, int RT>
 __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_stream_kernel(AttnArgs p, float* slots, int R) {
-    constexpr int E = KvElem<T>::E, NW = 16 / E, QS = kQSteps<D, T>, ES = (int)sizeof(T), LD = D + 4;
+    constexpr int E = KvElem<T>::E, NW = 16 / E, QS = kQSteps<D, T>, ES = (int)sizeof(T), LD = D + 4, PIECE = kPiece<RT>, RUNS = PIECE / 16;
     typedef typename KvElem<T>::vec vec;
     extern __shared__ char lds[];
     __shared__ int wave_sum[kWaves];
@@ -86,10 +88,11 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
     float* sum_o = (float*)(runs + kBatchRuns + 16);   // [kWaves][R][LD]
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int set = wave % RT, sub_of = wave / RT, RR = min(R, 32);       // the wavefront's row set, and which 32 tokens of a piece it has
     const int logp = p.b.log_page, P = 1 << logp;
     const int64_t page_bytes = (int64_t)P * D * ES;
 
-    const int64_t total = line_length<LIST>(p);
+    const int64_t total = line_length<LIST, RT>(p);
     const int64_t per = (total + gridDim.x - 1) / gridDim.x;
     int64_t at = per * blockIdx.x;
     const int64_t end = min(total, at + per);
@@ -104,7 +107,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
             int64_t c = 0;
             int tiles = 0;
             if (q < p.b.n_seq) {
-                const Part r = part_of<LIST>(p, q);
+                const Part r = part_of<LIST, RT>(p, q);
                 tiles = r.tiles;
                 c = (int64_t)r.tiles * r.pieces * p.n_kv;
             }
@@ -125,7 +128,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
     }
 
     while (at < end) {
-        const Part part = part_of<LIST>(p, s);
+        const Part part = part_of<LIST, RT>(p, s);
         const int64_t size = (int64_t)part.tiles * part.pieces * p.n_kv;
         if (rem >= size) {
             ++s;
@@ -139,23 +142,23 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         const int c1 = (int)min((int64_t)part.pieces, c0 + (end - at));
 
         int r0, r_end;
-        rows_of<LIST>(p, part, tile, r0, r_end);
+        rows_of<LIST, RT>(p, part, tile, r0, r_end);
         AttnRows<T, D> rows;
-        rows.load(p, head, part.first, part.n, part.len, r0 + col, r_end);
+        rows.load(p, head, part.first, part.n, part.len, r0 + set * 32 + col, r_end);
         AttnState<T, D> st;
         st.clear();
-        const int pos0 = part.len - part.n + r0 / p.G;                            // the first row's position, and the last one's
+        const int pos0 = part.len - part.n + (r0 + set * 32) / p.G;               // the set's first row's position; what the tile's last one sees
         const int hi = min(part.len - part.n + (r_end - 1) / p.G + 1, kv_blocks(p.b, part.len) << logp);
         const AttnSight sight(rows.pos, hi, p.window);
         const int32_t* list = LIST ? p.sel + ((int64_t)((tile0 + tile) / p.per_q) * p.n_kv + head) * p.top : nullptr;
         const int n_list = LIST ? p.top << (logp - 4) : 0;
-        for (int cb = c0; cb < c1; cb += kBatchRuns / 8) {
-            int n = min(c1 - cb, kBatchRuns / 8) * 8;
+        for (int cb = c0; cb < c1; cb += kBatchRuns / RUNS) {
+            int n = min(c1 - cb, kBatchRuns / RUNS) * RUNS;
             __syncthreads();                                                       // the last batch, the last tile's sums are read
             if (LIST) {
                 int there = 0;
                 for (int i0 = 0; i0 < n; i0 += kThreads) {
-                    const int j = cb * 8 + i0 + tid;
+                    const int j = cb * RUNS + i0 + tid;
                     const int blk = i0 + tid < n && j < n_list ? list[j >> (logp - 4)] : -1;
                     const int pos = blk >= 0 && blk < p.b.max_pages ? (blk << logp) + (j & (P / 16 - 1)) * 16 : 1 << 30;
                     const int page = pos < hi ? kv_page(p.b, s, blk) : -1;
@@ -164,22 +167,22 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                     if (page >= 0) runs[there + at] = int2{pos, page};
                     there += total;
                 }
-                n = (there + 7) & ~7;
+                n = (there + RUNS - 1) / RUNS * RUNS;
                 if (tid < n + 8 - there) runs[there + tid] = int2{1 << 30, -1};
             } else {
                 for (int i = tid; i < n + 8; i += kThreads) {
-                    int pos = i < n ? part.lo + cb * kPiece + i * 16 : 1 << 30;
+                    int pos = i < n ? part.lo + cb * PIECE + i * 16 : 1 << 30;
                     const int page = pos < hi ? kv_page(p.b, s, pos >> logp) : -1;
                     runs[i] = int2{page < 0 ? 1 << 30 : pos, page};
                 }
             }
             __syncthreads();
             if (n == 0) continue;
-            const int n_sub = n / 8;
+            const int n_sub = n / RUNS;
             // keys and values in VC parts of the channels: all of them ahead, or (fp32, 256 channels) only the first, as far as registers go
             constexpr int VC = D * ES > 512 ? 2 : 1, DC = D / 32 / VC, QC = QS / VC;
             vec kf[QC], vf[DC * NW];
-            int2 ra = runs[2 * wave], rb = runs[2 * wave + 1];
+            int2 ra = runs[2 * sub_of], rb = runs[2 * sub_of + 1];
             auto load_k = [&](int2 a, int2 b, int part) {
                 const int tk = kv_token<T>(col);
                 const int2 r = tk < 16 ? a : b;
@@ -222,8 +225,8 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                 }
                 const bool more = i + 1 < n_sub;
                 if (more) {
-                    ra = runs[(i + 1) * 8 + 2 * wave];
-                    rb = runs[(i + 1) * 8 + 2 * wave + 1];
+                    ra = runs[(i + 1) * RUNS + 2 * sub_of];
+                    rb = runs[(i + 1) * RUNS + 2 * sub_of + 1];
                     load_k(ra, rb, 0);
                 }
                 const bool masked = is_masked(a, b);
@@ -274,7 +277,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
             }
             if (odd)
                 for (int i = 0; i < n_sub; ++i) {
-                    const int2 a = runs[i * 8 + 2 * wave], b = runs[i * 8 + 2 * wave + 1];
+                    const int2 a = runs[i * RUNS + 2 * sub_of], b = runs[i * RUNS + 2 * sub_of + 1];
                     if (!is_masked(a, b)) continue;
 #pragma unroll 1
                     for (int j = 0; j < 32; ++j) {
@@ -287,19 +290,19 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                 }
         }
 
-        // the four wavefronts' sums
+        // the sums of a row set's wavefronts
         const float l = kv_pair_sum(st.l);
         if (half == 0) {
             sum_m[wave * 32 + col] = st.m;
             sum_l[wave * 32 + col] = l;
         }
         __syncthreads();
-        if (col < R) {
-            float m = sum_m[col];
+        if (col < RR) {
+            float m = sum_m[set * 32 + col];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sum_m[w * 32 + col]);
+            for (int w = RT; w < kWaves; w += RT) m = fmaxf(m, sum_m[(set + w) * 32 + col]);
             const float f = st.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.m - m);
-            float* dst = sum_o + (wave * R + col) * LD + half * 4;
+            float* dst = sum_o + (wave * RR + col) * LD + half * 4;
             // a wavefront that saw nothing has sums of zero; one whose sums hold a NaN keeps it through a factor of zero
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
@@ -313,16 +316,16 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         float* slot = slots + ((int64_t)blockIdx.x * 2 + (c0 == 0)) * ((int64_t)R * (D + 2));
         const int n_rows = min(R, r_end - r0);
         for (int i = tid; i < n_rows * (D / 4); i += kThreads) {
-            const int r = i / (D / 4), c = i % (D / 4) * 4;
-            float m = sum_m[r], lsum = 0.0f;
+            const int r = i / (D / 4), c = i % (D / 4) * 4, first = r / 32, rr = r & 31;
+            float m = sum_m[first * 32 + rr], lsum = 0.0f;
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sum_m[w * 32 + r]);
+            for (int w = RT; w < kWaves; w += RT) m = fmaxf(m, sum_m[(first + w) * 32 + rr]);
             kv_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float mw = sum_m[w * 32 + r];
-                lsum += sum_l[w * 32 + r] * kv_factor(mw, sum_l[w * 32 + r], m);
-                o += *(const kv_f32x4*)(sum_o + (w * R + r) * LD + c);
+            for (int w = 0; w < kWaves; w += RT) {
+                const int x = (first + w) * 32 + rr;
+                lsum += sum_l[x] * kv_factor(sum_m[x], sum_l[x], m);
+                o += *(const kv_f32x4*)(sum_o + ((first + w) * RR + rr) * LD + c);
             }
             if (whole) {
                 const int t = (r0 + r) / p.G;
@@ -346,11 +349,11 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
 
 // Joins the runs of the row tiles that more than one workgroup had: workgroups per tile and head that take
 // 32 channels of 4 rows at a time; eight threads have a row's channels, and eight such share its runs.
-template <typename T, int D, bool LIST>
+template <typename T, int D, bool LIST, int RT>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const float* slots, int R, int groups) {
     __shared__ float part_o[kThreads][4], part_m[kThreads], part_l[kThreads];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int64_t total = line_length<LIST>(p);
+    const int64_t total = line_length<LIST, RT>(p);
     const int64_t per = (total + groups - 1) / groups;
     // the tile's place on the line
     const int head = blockIdx.x % p.n_kv;
@@ -361,7 +364,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const f
         int64_t c = 0;
         int tiles = 0;
         if (q < p.b.n_seq) {
-            const Part r = part_of<LIST>(p, q);
+            const Part r = part_of<LIST, RT>(p, q);
             tiles = r.tiles;
             c = (int64_t)r.tiles * r.pieces * p.n_kv;
         }
@@ -379,12 +382,12 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const f
         run += __shfl(incl, 63);
     }
     if (s < 0) return;
-    const Part part = part_of<LIST>(p, s);
+    const Part part = part_of<LIST, RT>(p, s);
     const int64_t a = run + (want * p.n_kv + head) * part.pieces, b = a + part.pieces;
     const int w0 = (int)(a / per), w1 = (int)((b - 1) / per);
     if (w0 == w1) return;
     int r0, r_end;
-    rows_of<LIST>(p, part, (int)want, r0, r_end);
+    rows_of<LIST, RT>(p, part, (int)want, r0, r_end);
     const int n_rows = min(R, r_end - r0);
     const int64_t stride = (int64_t)R * (D + 2);
     const int k = tid >> 5;
@@ -429,16 +432,16 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const f
     }
 }
 
-template <typename T, int D, bool LIST>
+template <typename T, int D, bool LIST, int RT>
 int launch(const AttnArgs& p, int64_t tiles, int R, float* ws, hipStream_t st) {
     static S3LdsOnce once;
-    const int bytes = kWaves * 32 * 8 + (kBatchRuns + 16) * 8 + kWaves * R * (D + 4) * 4;
-    if (int rc = s3_allow_lds(once, (const void*)attn_stream_kernel<T, D, LIST>, kWaves * 32 * 8 + (kBatchRuns + 16) * 8 + kWaves * 32 * (D + 4) * 4)) return rc;
+    const int bytes = kWaves * 32 * 8 + (kBatchRuns + 16) * 8 + kWaves * min(R, 32) * (D + 4) * 4;
+    if (int rc = s3_allow_lds(once, (const void*)attn_stream_kernel<T, D, LIST, RT>, kWaves * 32 * 8 + (kBatchRuns + 16) * 8 + kWaves * 32 * (D + 4) * 4)) return rc;
     const int64_t join = tiles * p.n_kv;
     if (join >= (int64_t)1 << 22) return s3_fail(S3_EINVAL, "attention: too many tokens in one call");
-    hipLaunchKernelGGL((attn_stream_kernel<T, D, LIST>), dim3(kRunGroups), dim3(kThreads), bytes, st, p, ws, R);
+    hipLaunchKernelGGL((attn_stream_kernel<T, D, LIST, RT>), dim3(kRunGroups), dim3(kThreads), bytes, st, p, ws, R);
     S3_HIP(hipGetLastError());
-    hipLaunchKernelGGL((attn_join_kernel<T, D, LIST>), dim3((unsigned)join, (unsigned)max((int64_t)1, min(4096 / join, (int64_t)(D / 32 * ((R + 3) / 4))))), dim3(kThreads), 0, st, p, ws, R, kRunGroups);
+    hipLaunchKernelGGL((attn_join_kernel<T, D, LIST, RT>), dim3((unsigned)join, (unsigned)max((int64_t)1, min(4096 / join, (int64_t)(D / 32 * ((R + 3) / 4))))), dim3(kThreads), 0, st, p, ws, R, kRunGroups);
     S3_HIP(hipGetLastError());
     return S3_OK;
 }
@@ -448,8 +451,12 @@ int launch(const AttnArgs& p, int64_t tiles, int R, float* ws, hipStream_t st) {
 size_t s3_attn_stream_workspace(int d_head, int R) { return s3_align((size_t)kRunGroups * 2 * R * (d_head + 2) * 4); }
 
 int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st) {
-#define S3_STREAM(T, D) (p.sel ? launch<T, D, true>(p, tiles, R, (float*)ws, st) : launch<T, D, false>(p, tiles, R, (float*)ws, st))
+    const int rt = R <= 32 ? 1 : R <= 64 ? 2 : 4;
+#define S3_STREAM2(T, D, L) \
+    (rt == 1 ? launch<T, D, L, 1>(p, tiles, R, (float*)ws, st) : rt == 2 ? launch<T, D, L, 2>(p, tiles, R, (float*)ws, st) : launch<T, D, L, 4>(p, tiles, R, (float*)ws, st))
+#define S3_STREAM(T, D) (p.sel ? S3_STREAM2(T, D, true) : S3_STREAM2(T, D, false))
     if (c->dtype == S3_BF16) return c->d_head == 64 ? S3_STREAM(__bf16, 64) : c->d_head == 128 ? S3_STREAM(__bf16, 128) : S3_STREAM(__bf16, 256);
     return c->d_head == 64 ? S3_STREAM(float, 64) : c->d_head == 128 ? S3_STREAM(float, 128) : S3_STREAM(float, 256);
 #undef S3_STREAM
+#undef S3_STREAM2
 }

@@ -20,14 +20,14 @@ int check_ws(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
     return S3_OK;
 }
 
-// The most rows of one sequence (or tile of listed blocks) that the streaming kernel takes, 32 at a time; the tiled kernel has more.
-// Every 32 rows read the keys and values once more there, while the tiled kernel's 256 rows a workgroup stand mostly empty.  us with the
-// limit at 32 / at the one taken: 16 tokens x 4 heads at 32768 tokens, d_head 64: 42 / 25, fp32: 171 / 116; tiles of 16 queries x 4 heads over
-// 64 listed blocks, bf16: 343 / 264, d_head 64: 276 / 161; but 8 x 16 tokens at 8000 in bf16 with d_head 128: 66 / 107, so 32 there.
-// fp32, 8 x 32 tokens x 4 heads at 8000: 579 / 396 with 128.
+// The most rows of one sequence (or tile of listed blocks) that the streaming kernel takes; the tiled kernel has more, whose 256 rows a
+// workgroup would stand mostly empty below.  us in the tiled / in the streaming kernel, 32 query heads over 8: 16 tokens of one sequence at
+// 32768 with d_head 64: 42 / 27, of eight at 8000 with 256: 258 / 208, in fp32: 355 / 217 (32 tokens: 579 / 375); tiles of 16
+// queries over 64 listed blocks of 512: 343 / 240, d_head 64: 276 / 154.  But bf16 with d_head 128, eight sequences: 66 / 73, where the tiled
+// kernel's rate is best.
 int few_rows(const s3_kv_cache* c, bool list) {
     if (c->dtype == S3_FP32) return c->d_head == 128 ? 128 : 64;
-    return list || c->d_head == 64 ? 64 : 32;
+    return list || c->d_head != 128 ? 64 : 32;
 }
 
 // How a call is shared out.
@@ -42,15 +42,18 @@ struct Plan {
         limit = few_rows(c, q_block != 0);
         qb = min(q_block, max(b->n_tokens, 1));
         const int64_t most = (int64_t)(q_block ? qb : min(max(b->max_new, 1), max(b->n_tokens, 1))) * G;
+        many = most > limit;
+        if (many && !q_block) limit = 32;                     // beside chunks the short ones are single tokens, mostly
         // no sequence is a short one if even the others at their longest leave more rows for it
         const bool all_long = b->n_tokens > (int64_t)(b->n_seq - 1) * b->max_new + limit / G;
-        few = most <= limit || (!q_block && !all_long);
-        many = most > limit;
-        R = (int)min(most, (int64_t)32);
+        few = !many || (!q_block && !all_long);
+        // row tiles of 32, 64 or 128 rows: one whenever they go into one
+        R = (int)min(most, (int64_t)limit);
+        const int tile = R <= 32 ? 32 : R <= 64 ? 64 : 128;
         few_ws = few ? s3_attn_stream_workspace(c->d_head, R) : 0;
         const int rows = s3_attn_tile_rows(c);
-        per_q = !q_block ? 1 : (int)((most + (many ? rows : 32) - 1) / (many ? rows : 32));
-        few_tiles = q_block ? s3_block_tiles(b, q_block) * per_q : min(((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * 31) / 32, (int64_t)b->n_seq * (limit / 32));
+        per_q = !q_block ? 1 : (int)((most + (many ? rows : tile) - 1) / (many ? rows : tile));
+        few_tiles = q_block ? s3_block_tiles(b, q_block) * per_q : min(((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * (tile - 1)) / tile, (int64_t)b->n_seq);
         many_tiles = !many ? 0 : q_block ? s3_block_tiles(b, q_block) * per_q
                                          : ((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * (rows - 1)) / rows;
         const int64_t units = many_tiles * c->n_kv_heads, tokens = q_block ? (int64_t)top_b * c->page_size : b->max_kv;
