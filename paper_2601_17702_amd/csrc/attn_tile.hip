@@ -303,7 +303,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     }
 }
 
-// Joins the splits of a row tile: a thread per row and 4 channels.
+// Joins the parts of a row tile: a thread per row and 4 channels at a time.
 template <typename T, int D, bool LIST, int ROWS>
 __global__ __launch_bounds__(256) void attn_tile_join_kernel(AttnArgs p, TileArgs ta) {
     const int head = blockIdx.x % p.n_kv, tile = blockIdx.x / p.n_kv;
@@ -318,23 +318,28 @@ __global__ __launch_bounds__(256) void attn_tile_join_kernel(AttnArgs p, TileArg
     }
     const int64_t stride = (int64_t)ROWS * (D + 2);
     const float* slots = ta.slots + (int64_t)(tile * p.n_kv + head) * ta.n_split * stride;
-    const int x = blockIdx.y * 256 + threadIdx.x, row = x / (D / 4), c = x % (D / 4) * 4;
-    if (row >= ROWS || r0 + row >= r_end) return;
-    float m = -INFINITY, l = 0.0f;
-    kv_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int w = 0; w < ta.n_split; ++w) m = fmaxf(m, slots[w * stride + ROWS * D + row]);
-    for (int w = 0; w < ta.n_split; ++w) {
-        const float mw = slots[w * stride + ROWS * D + row], lw = slots[w * stride + ROWS * D + ROWS + row];
-        const float f = kv_factor(mw, lw, m);
-        l += lw * f;
-        o += *(const kv_f32x4*)(slots + w * stride + row * D + c) * f;
+    const int rows = min(ROWS, r_end - r0);
+    for (int x = blockIdx.y * 256 + threadIdx.x; x < rows * (D / 4); x += gridDim.y * 256) {
+        const int row = x / (D / 4), c = x % (D / 4) * 4;
+        float m = -INFINITY, l = 0.0f;
+        kv_f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int w = 0; w < ta.n_split; ++w) {
+            const float* slot = slots + w * stride;
+            const float mw = slot[ROWS * D + row], lw = slot[ROWS * D + ROWS + row];
+            const kv_f32x4 ow = *(const kv_f32x4*)(slot + row * D + c);
+            const float m2 = fmaxf(m, mw), fa = kv_factor(m, l, m2), fb = kv_factor(mw, lw, m2);
+            m = m2;
+            l = l * fa + lw * fb;
+            o = o * fa + ow * fb;
+        }
+        const int t = (r0 + row) / p.G;
+        const int64_t at = (int64_t)(first + t) * p.n_q + head * p.G + (r0 + row - t * p.G);
+        const float inv = kv_inverse(l);
+        typedef __attribute__((ext_vector_type(4))) T four;
+        *(four*)(p.out + (at * D + c) * (int)sizeof(T)) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
+        if (p.lse && c == 0) p.lse[at] = kv_lse(m, l);
     }
-    const int t = (r0 + row) / p.G;
-    const int64_t at = (int64_t)(first + t) * p.n_q + head * p.G + (r0 + row - t * p.G);
-    const float inv = kv_inverse(l);
-    typedef __attribute__((ext_vector_type(4))) T four;
-    *(four*)(p.out + (at * D + c) * (int)sizeof(T)) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
-    if (p.lse && c == 0) p.lse[at] = kv_lse(m, l);
 }
 
 // Wavefronts and row sets of the builds: 256 rows a workgroup; 128 where the operands of 256 do not fit the registers.
@@ -355,7 +360,7 @@ int launch(const AttnArgs& p, const TileArgs& ta, hipStream_t st) {
     hipLaunchKernelGGL((attn_tile_kernel<T, D, LIST, RS, W>), dim3((unsigned)units, ta.n_split), dim3(W * 64), bytes, st, p, ta);
     S3_HIP(hipGetLastError());
     if (ta.n_split > 1) {
-        hipLaunchKernelGGL((attn_tile_join_kernel<T, D, LIST, ROWS>), dim3((unsigned)units, ROWS * (D / 4) / 256), dim3(256), 0, st, p, ta);
+        hipLaunchKernelGGL((attn_tile_join_kernel<T, D, LIST, ROWS>), dim3((unsigned)units, units < 64 ? 32 : 8), dim3(256), 0, st, p, ta);
         S3_HIP(hipGetLastError());
     }
     return S3_OK;
