@@ -352,7 +352,7 @@ typedef struct {
  * q_start[s] .. q_start[s + 1] - 1 of the call's arrays; they are the LAST of its kv_len[s] tokens (new ones
  * counted), so row i of n stands at position kv_len[s] - n + i.  Position p lies in slot p % page_size of page
  * block_table[s * table_stride + p / page_size].
- *   q_start      [n_seq + 1] int32, ascending, q_start[n_seq] <= n_tokens; NULL: one new token per sequence, n_tokens == n_seq
+ *   q_start      [n_seq + 1] int32, never descending, q_start[n_seq] <= n_tokens; NULL: one new token per sequence, n_tokens == n_seq
  *   kv_len       [n_seq] int32;  block_table [n_seq][table_stride] int32, max_pages entries of a row used
  *   max_new, max_kv   bounds of a sequence's new tokens and of kv_len: they size workspaces and share out the work, and
  *                what goes beyond them may be left out

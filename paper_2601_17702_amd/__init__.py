@@ -518,7 +518,7 @@ class KVCache:
         rows, width = block_table.shape
         stride, inner = block_table.stride()
         assert i32 is _torch().int32 and block_table.dtype is i32 and kv_len.is_cuda and block_table.is_cuda
-        assert rows == n_seq and (inner == 1 or width <= 1) and kv_len.is_contiguous()
+        assert rows == n_seq and (inner == 1 or width <= 1) and (stride >= width or rows <= 1) and kv_len.is_contiguous()
         qs = 0
         if q_start is not None:
             assert q_start.dtype is i32 and q_start.is_cuda and q_start.shape == (n_seq + 1,) and q_start.is_contiguous()
@@ -526,7 +526,7 @@ class KVCache:
         else:
             assert n_tokens == n_seq
             max_new = 1
-        return _KV_BATCH.pack(qs, kv_len.data_ptr(), block_table.data_ptr(), stride if rows > 1 and stride > width else width, n_seq, n_tokens, width,
+        return _KV_BATCH.pack(qs, kv_len.data_ptr(), block_table.data_ptr(), stride if rows > 1 else width, n_seq, n_tokens, width,
                               n_tokens if max_new is None else max_new, width * self.page_size if max_kv is None else max_kv)
 
     def _rows(self, x, heads=None):

@@ -147,11 +147,12 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         rows.load(p, head, part.first, part.n, part.len, r0 + set * 32 + col, r_end);
         AttnState<T, D> st;
         st.clear();
-        const int pos0 = part.len - part.n + (r0 + set * 32) / p.G;               // the set's first row's position; what the tile's last one sees
-        const int hi = min(part.len - part.n + (r_end - 1) / p.G + 1, kv_blocks(p.b, part.len) << logp);
+        const int pos0 = part.len - part.n + (r0 + set * 32) / p.G;               // the set's first row's position
+        const int last = part.len - part.n + (r_end - 1) / p.G;                   // the last row's; its tokens end at hi
+        const int hi = min(last + 1, kv_blocks(p.b, part.len) << logp);
         const AttnSight sight(rows.pos, hi, p.window);
         const int32_t* list = LIST ? p.sel + ((int64_t)((tile0 + tile) / p.per_q) * p.n_kv + head) * p.top : nullptr;
-        const int n_list = LIST ? p.top << (logp - 4) : 0;
+        const int n_list = LIST && (tile0 + tile) / p.per_q < p.lists ? p.top << (logp - 4) : 0;
         for (int cb = c0; cb < c1; cb += kBatchRuns / RUNS) {
             int n = min(c1 - cb, kBatchRuns / RUNS) * RUNS;
             __syncthreads();                                                       // the last batch, the last tile's sums are read
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
             // some row does not see some token of the 32
             auto is_masked = [&](int2 a, int2 b) {
                 const int far = max(a.x, b.x) + 15;
-                return far > pos0 || far >= hi || (p.window && min(a.x, b.x) <= hi - 1 - p.window);
+                return far > pos0 || far >= hi || (p.window && min(a.x, b.x) <= last - p.window);
             };
             bool odd = false;
             load_k(ra, rb, 0);

@@ -1,9 +1,14 @@
-// Attention of many rows: chunks of new tokens (and tiles of listed blocks) with more than 32 rows per key/value head.
+// Attention of many rows: chunks of new tokens (and tiles of listed blocks) with more rows per key/value head than attn_stream.hip takes.
 //
-// The two products bound it.  A workgroup has kWaves wavefronts of RS * 32 rows each, the rows of a head's G query heads token by
+// The two products bound it.  A workgroup has WAVES wavefronts of RS * 32 rows each, the rows of a head's G query heads token by
 // token, and walks over the tokens that some row sees, KT at a time: keys and values come through registers into one of two LDS
 // buffers while the other is worked on, in the layout that they have in the cache, which is the one in which every operand read
-// is 16 bytes a lane from neighbouring places (no bank conflicts, no transposition).
+// is 16 bytes a lane from neighbouring places (no bank conflicts, no transposition).  LDS feeds 128 bytes a clock: with 32 rows a wavefront
+// all of it at the matrix units' full rate, which the card's clock does not let them reach (below).
+//
+// Measured: 2048 tokens at 131072, 32 query heads over 8, d_head 128, bf16 (4.4 TFLOP): 4.1 ms, 1050 TFLOP/s, where a large library product
+// reaches 1159 on the card.  MFMAs are busy 48 % of the cycles at 1.9 GHz; a variant half as fast ran at 2.33 GHz, so the clock gives
+// way before the units are full.  d_head 256 has one wavefront a SIMD (512 registers) and 43 % of that product's rate, fp32 70 % of fp32's.
 #include "attn_launch.h"
 
 namespace {
@@ -69,7 +74,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     }
 
     // what some row of the workgroup does not see: such steps are masked, and their values looked at
-    const int wg0 = len - n + r0 / p.G;
+    const int wg0 = len - n + r0 / p.G, wg1 = len - n + (r_end - 1) / p.G;
     auto partly = [&](int2 span, int first_pos, int last_pos) {
         return span.y > first_pos || span.y >= hi || (p.window && span.x <= last_pos - p.window);
     };
@@ -101,7 +106,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     // Where some row does not see some token of the step, values that are not finite leave the buffer: their products with a weight of zero
     // would be NaN.  The rows that do see them get them from memory, one token at a time (rare); what lies past the end is zero.
     auto store = [&](int t) {
-        if (partly(span_of(t), wg0, hi - 1)) {
+        if (partly(span_of(t), wg0, wg1)) {
             unsigned big = 0;
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
@@ -250,7 +255,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if (partly(span, wg0, hi - 1) && odd_step[t & 1] == t)
+                if (partly(span, wg0, wg1) && odd_step[t & 1] == t)
 #pragma unroll 1
                     for (int tk = 0; tk < KT; ++tk) {
                         const int4 r = runs[t * (KT / 16) + tk / 16];

@@ -91,7 +91,7 @@ extern "C" int s3_paged_attention(const s3_kv_cache* c, const s3_kv_batch* b, co
     if (int rc = check_ws(fn, ws, ws_bytes, plan.bytes())) return rc;
     const int es = c->dtype == S3_BF16 ? 2 : 4;
     AttnArgs p{s3_kv_batch_args(c, b), (const char*)q, (char*)out, lse, (const char*)c->k, (const char*)c->v, nullptr, q_ts * es,
-               q_hs * es, c->n_kv_heads, plan.G, n_q, window, 0, 0, 1, scale * 1.4426950408889634f, 0};
+               q_hs * es, c->n_kv_heads, plan.G, n_q, window, 0, 0, 1, 0, scale * 1.4426950408889634f, 0};
     return run(fn, c, b, p, plan, ws, (hipStream_t)stream);
 }
 
@@ -114,6 +114,6 @@ extern "C" int s3_block_attention(const s3_kv_cache* c, const s3_kv_batch* b, co
     if (int rc = check_ws(fn, ws, ws_bytes, plan.bytes())) return rc;
     const int es = c->dtype == S3_BF16 ? 2 : 4;
     AttnArgs p{s3_kv_batch_args(c, b), (const char*)q, (char*)out, lse, (const char*)c->k, (const char*)c->v, sel, q_ts * es,
-               q_hs * es, c->n_kv_heads, plan.G, n_q, 0, 0, top_b, 1, scale * 1.4426950408889634f, 0};
+               q_hs * es, c->n_kv_heads, plan.G, n_q, 0, 0, top_b, 1, (int)s3_block_tiles(b, q_block), scale * 1.4426950408889634f, 0};
     return run(fn, c, b, p, plan, ws, (hipStream_t)stream);
 }

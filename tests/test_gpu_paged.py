@@ -57,6 +57,16 @@ def test_attention_window(dtype, d, P, hq, hkv, new, kv, window):
     paged.check(pr, o, lse, paged.attend(pr, window=window))
 
 
+@pytest.mark.parametrize("dtype,new,window", [("bf16", 1, 0), ("bf16", 1, 40), ("bf16", 90, 0), ("bf16", 90, 30), ("fp32", 70, 50), ("fp32", 2, 300)])
+def test_sequences_longer_than_their_table(dtype, new, window):
+    """Tokens whose block lies behind the table's last one are masked; positions and windows are still those of the whole sequence."""
+    pr = paged.Problem(18, dtype, 64, 16, 4, 2, [new, 3], [250, 20])
+    pr.table = pr.table[:, :13].contiguous()                          # 208 of 250 positions
+    kv_len, table = pr.args()
+    o, lse = pr.cache().attention(pr.q.cuda(), kv_len, table, q_start=pr.q_start.cuda(), window=window, want_lse=True)
+    paged.check(pr, o, lse, paged.attend(pr, window=window))
+
+
 @pytest.mark.parametrize("new,kv", [([1, 1], [2000, 5]), ([40, 40], [100, 2000]), ([200], [1500])])
 def test_attention_of_large_scores(new, kv):
     """Scores in the hundreds: a row's weight sits on one token or few, its maximum moves many times."""
