@@ -1,6 +1,6 @@
 // Attention of many rows: chunks of new tokens (and tiles of listed blocks) with more rows per key/value head than attn_stream.hip takes.
 //
-// The two products bound it.  A workgroup has WAVES wavefronts of RS * 32 rows each, the rows of a head's G query heads token by
+// The two products bound it.  A workgroup has WAVES wavefronts of 32 rows each, the rows of a head's G query heads token by
 // token, and walks over the tokens that some row sees, KT at a time: keys and values come through registers into one of two LDS
 // buffers while the other is worked on, in the layout that they have in the cache, which is the one in which every operand read
 // is 16 bytes a lane from neighbouring places (no bank conflicts, no transposition).  LDS feeds 128 bytes a clock: with 32 rows a wavefront
@@ -22,10 +22,10 @@ struct TileArgs {
     int n_split, tiles;       // row tiles that there can be
 };
 
-template <typename T, int D, bool LIST, int RS, int WAVES>
+template <typename T, int D, bool LIST, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnArgs p, TileArgs ta) {
     constexpr int E = KvElem<T>::E, NW = 16 / E, QS = kQSteps<D, T>, ES = (int)sizeof(T), KT = kTokens<T, D>, NS = KT / 32;
-    constexpr int THREADS = WAVES * 64, ROWS = WAVES * RS * 32;
+    constexpr int THREADS = WAVES * 64, ROWS = WAVES * 32;
     constexpr int PIECES = KT * D / E, LOADS = PIECES / THREADS;       // 16-byte pieces of a buffer's keys (and of its values)
     static_assert(PIECES % THREADS == 0, "every thread has as many pieces");
     typedef typename KvElem<T>::vec vec;
@@ -62,16 +62,14 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     const int split = blockIdx.y;
     const int t0 = (int)((int64_t)steps * split / ta.n_split), t1 = (int)((int64_t)steps * (split + 1) / ta.n_split);
 
-    const int rw = r0 + wave * (RS * 32);                             // this wavefront's first row
+    const int rw = r0 + wave * 32;                             // this wavefront's first row
     const int pos0 = len - n + rw / p.G;                              // its position, and the last row's
-    const int pos1 = rw < r_end ? len - n + (min(rw + RS * 32, r_end) - 1) / p.G : -1;
-    AttnRows<T, D> rows[RS];
-    AttnState<T, D> st[RS];
-#pragma unroll
-    for (int r = 0; r < RS; ++r) {
-        rows[r].load(p, head, first, n, len, rw + r * 32 + col, r_end);
-        st[r].clear();
-    }
+    const int pos1 = rw < r_end ? len - n + (min(rw + 32, r_end) - 1) / p.G : -1;
+    AttnRows<T, D> rows;
+    AttnState<T, D> st;
+    rows.load(p, head, first, n, len, rw + col, r_end);
+    st.clear();
+    const AttnSight sight(rows.pos, hi, p.window);
 
     // what some row of the workgroup does not see: such steps are masked, and their values looked at
     const int wg0 = len - n + r0 / p.G, wg1 = len - n + (r_end - 1) / p.G;
@@ -178,26 +176,21 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
             const int2 span = span_of(t);
             if (span.x <= pos1) {                                     // some row of the wavefront sees some token
                 // kAhead operands are read ahead of the products that take them (the compiler's own order waits for each)
-                constexpr int kAhead = 6, kProducts = RS * (E == 8 ? 1 : 4), DT = D / 32;
-                kv_f32x16 sc[RS][NS];
+                constexpr int kAhead = 6, kProducts = E == 8 ? 1 : 4, DT = D / 32;
+                kv_f32x16 sc[NS];
 #pragma unroll
                 for (int x = 0; x < NS; ++x) {
 #pragma unroll
-                    for (int r = 0; r < RS; ++r)
+                    for (int i = 0; i < 16; ++i) sc[x][i] = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) sc[r][x][i] = 0.0f;
-#pragma unroll
-                    for (int q = 0; q < QS; ++q) {
-                        const vec kf = *(const vec*)(kb + ((2 * q + half) * KT + x * 32 + kv_token<T>(col)) * 16);
-#pragma unroll
-                        for (int r = 0; r < RS; ++r) sc[r][x] = kv_mma(kf, rows[r].q[q], sc[r][x]);
-                    }
+                    for (int q = 0; q < QS; ++q)
+                        sc[x] = kv_mma(*(const vec*)(kb + ((2 * q + half) * KT + x * 32 + kv_token<T>(col)) * 16), rows.q[q], sc[x]);
                 }
                 auto values = [&](int y, vec (&v)[DT]) {              // operands of E tokens a lane
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) v[dt] = *(const vec*)(vb + ((2 * y + half) * D + dt * 32 + col) * 16);
                 };
-                vec v[2][DT], w[2][RS];
+                vec v[2][DT], w[2];
                 values(0, v[0]);
                 __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
@@ -209,48 +202,36 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
                 if (masked) {
                     asm volatile("");                                 // stays a branch: most steps skip it
 #pragma unroll
-                    for (int r = 0; r < RS; ++r) {
-                        const AttnSight sight(rows[r].pos, hi, p.window);
+                    for (int x = 0; x < NS; ++x)
 #pragma unroll
-                        for (int x = 0; x < NS; ++x)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const int tk = x * 32 + 2 * E * (i / E) + E * half + i % E;
-                                sc[r][x][i] = sight.sees(runs[t * (KT / 16) + (x * 32 + 2 * E * (i / E)) / 16].w + (tk & 15)) ? sc[r][x][i] : -INFINITY;
-                            }
-                    }
+                        for (int i = 0; i < 16; ++i) {
+                            const int tk = x * 32 + 2 * E * (i / E) + E * half + i % E;
+                            sc[x][i] = sight.sees(runs[t * (KT / 16) + (x * 32 + 2 * E * (i / E)) / 16].w + (tk & 15)) ? sc[x][i] : -INFINITY;
+                        }
                 }
-                float sub[RS];
+                float top = sc[0][0];
 #pragma unroll
-                for (int r = 0; r < RS; ++r) {
-                    float x = sc[r][0][0];
+                for (int y = 0; y < NS; ++y)
 #pragma unroll
-                    for (int y = 0; y < NS; ++y)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x = fmaxf(x, sc[r][y][i]);
-                    sub[r] = st[r].advance(x, p.sl);
-                }
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[y][i]);
+                const float sub = st.advance(top, p.sl);
                 // the weights and operands of the next tokens are made while these tokens' products run
-#pragma unroll
-                for (int r = 0; r < RS; ++r) w[0][r] = st[r].weights(sc[r][0], 0, p.sl, sub[r]);
+                w[0] = st.weights(sc[0], 0, p.sl, sub);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int y = 0; y < NS * NW; ++y) {
                     if (y + 1 < NS * NW) {
                         values(y + 1, v[(y + 1) & 1]);
-#pragma unroll
-                        for (int r = 0; r < RS; ++r) w[(y + 1) & 1][r] = st[r].weights(sc[r][(y + 1) / NW], (y + 1) % NW, p.sl, sub[r]);
+                        w[(y + 1) & 1] = st.weights(sc[(y + 1) / NW], (y + 1) % NW, p.sl, sub);
                     }
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                        for (int r = 0; r < RS; ++r) st[r].o[dt] = kv_mma(v[y & 1][dt], w[y & 1][r], st[r].o[dt]);
+                    for (int dt = 0; dt < DT; ++dt) st.o[dt] = kv_mma(v[y & 1][dt], w[y & 1], st.o[dt]);
                     if (y + 1 < NS * NW) {
                         __builtin_amdgcn_sched_group_barrier(0x100, DT, 0);
 #pragma unroll
                         for (int dt = 0; dt < DT; ++dt) {
                             __builtin_amdgcn_sched_group_barrier(0x8, kProducts, 0);
-                            __builtin_amdgcn_sched_group_barrier(0x402, (RS * E * 7 / 2 + DT - 1) / DT, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x402, (E * 7 / 2 + DT - 1) / DT, 0);
                         }
                     }
                     __builtin_amdgcn_sched_barrier(0);
@@ -262,9 +243,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
                         const int slot = r.z + (tk & 15);
                         if (r.w + (tk & 15) >= hi) continue;
                         const char* src = p.v + ((int64_t)(((uint64_t)(unsigned)r.y << 32) | (unsigned)r.x)) + slot / E * (D * 16) + slot % E * ES;
-#pragma unroll
-                        for (int x = 0; x < RS; ++x)
-                            st[x].add_nonfinite(AttnSight(rows[x].pos, hi, p.window).sees(r.w + (tk & 15)), [&](int c) { return (float)*(const T*)(src + c * 16); });
+                        st.add_nonfinite(sight.sees(r.w + (tk & 15)), [&](int c) { return (float)*(const T*)(src + c * 16); });
                     }
             }
             if (more) store(t + 1);
@@ -272,39 +251,36 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
         }
     }
 
-#pragma unroll
-    for (int r = 0; r < RS; ++r) {
-        const float l = kv_pair_sum(st[r].l);
-        const int row = wave * (RS * 32) + r * 32 + col;
-        if (ta.n_split > 1) {
-            float* slot = ta.slots + ((int64_t)(tile * p.n_kv + head) * ta.n_split + split) * ((int64_t)ROWS * (D + 2));
-            if (r0 + row < r_end) {
-#pragma unroll
-                for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                    for (int a = 0; a < 4; ++a)
-                        *(kv_f32x4*)(slot + row * D + dt * 32 + a * 8 + half * 4) =
-                            kv_f32x4{st[r].o[dt][4 * a], st[r].o[dt][4 * a + 1], st[r].o[dt][4 * a + 2], st[r].o[dt][4 * a + 3]};
-                if (half == 0) {
-                    slot[ROWS * D + row] = st[r].m;
-                    slot[ROWS * D + ROWS + row] = l;
-                }
-            }
-        } else if (rows[r].row >= 0) {
-            const float inv = kv_inverse(l);
-            char* out = p.out + rows[r].row * (D * ES);
+    const float l = kv_pair_sum(st.l);
+    if (ta.n_split > 1) {
+        const int row = wave * 32 + col;
+        float* slot = ta.slots + ((int64_t)(tile * p.n_kv + head) * ta.n_split + split) * ((int64_t)ROWS * (D + 2));
+        if (r0 + row < r_end) {
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    typedef __attribute__((ext_vector_type(4))) T four;
-                    four x;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = (T)(st[r].o[dt][a * 4 + e] * inv);
-                    *(four*)(out + (dt * 32 + a * 8 + half * 4) * ES) = x;
-                }
-            if (p.lse && half == 0) p.lse[rows[r].row] = kv_lse(st[r].m, l);
+                for (int a = 0; a < 4; ++a)
+                    *(kv_f32x4*)(slot + row * D + dt * 32 + a * 8 + half * 4) =
+                        kv_f32x4{st.o[dt][4 * a], st.o[dt][4 * a + 1], st.o[dt][4 * a + 2], st.o[dt][4 * a + 3]};
+            if (half == 0) {
+                slot[ROWS * D + row] = st.m;
+                slot[ROWS * D + ROWS + row] = l;
+            }
         }
+    } else if (rows.row >= 0) {
+        const float inv = kv_inverse(l);
+        char* out = p.out + rows.row * (D * ES);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                typedef __attribute__((ext_vector_type(4))) T four;
+                four x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = (T)(st.o[dt][a * 4 + e] * inv);
+                *(four*)(out + (dt * 32 + a * 8 + half * 4) * ES) = x;
+            }
+        if (p.lse && half == 0) p.lse[rows.row] = kv_lse(st.m, l);
     }
 }
 
@@ -347,22 +323,21 @@ __global__ __launch_bounds__(256) void attn_tile_join_kernel(AttnArgs p, TileArg
     }
 }
 
-// Wavefronts and row sets of the builds: 256 rows a workgroup; 128 where the operands of 256 do not fit the registers.
-template <typename T, int D> constexpr int kSets = 1;
+// Wavefronts of the builds: 256 rows a workgroup; 128 where two wavefronts of a SIMD have too few registers.
 template <typename T, int D> constexpr int kWaves = D * (int)sizeof(T) > 256 ? 4 : 8;
-template <typename T, int D> constexpr int kRows = kSets<T, D> * kWaves<T, D> * 32;
+template <typename T, int D> constexpr int kRows = kWaves<T, D> * 32;
 
 int rows_of(const s3_kv_cache* c) { return c->d_head * (c->dtype == S3_BF16 ? 2 : 4) > 256 ? 128 : 256; }
 
 template <typename T, int D, bool LIST>
 int launch(const AttnArgs& p, const TileArgs& ta, hipStream_t st) {
-    constexpr int RS = kSets<T, D>, W = kWaves<T, D>, ROWS = kRows<T, D>;
+    constexpr int W = kWaves<T, D>, ROWS = kRows<T, D>;
     constexpr int bytes = 4 * kTokens<T, D> * D * (int)sizeof(T) + kBatchRuns * 16 + kBatchRuns * 16 / kTokens<T, D> * 8 + 8;
     static S3LdsOnce once;
-    if (int rc = s3_allow_lds(once, (const void*)attn_tile_kernel<T, D, LIST, RS, W>, bytes)) return rc;
+    if (int rc = s3_allow_lds(once, (const void*)attn_tile_kernel<T, D, LIST, W>, bytes)) return rc;
     const int64_t units = (int64_t)ta.tiles * p.n_kv;
     if (units >= (int64_t)1 << 22) return s3_fail(S3_EINVAL, "attention: too many tokens in one call");
-    hipLaunchKernelGGL((attn_tile_kernel<T, D, LIST, RS, W>), dim3((unsigned)units, ta.n_split), dim3(W * 64), bytes, st, p, ta);
+    hipLaunchKernelGGL((attn_tile_kernel<T, D, LIST, W>), dim3((unsigned)units, ta.n_split), dim3(W * 64), bytes, st, p, ta);
     S3_HIP(hipGetLastError());
     if (ta.n_split > 1) {
         hipLaunchKernelGGL((attn_tile_join_kernel<T, D, LIST, ROWS>), dim3((unsigned)units, units < 64 ? 32 : 8), dim3(256), 0, st, p, ta);
