@@ -6,8 +6,8 @@
 // chip idle (few tiles, long contexts) or does not fit LDS, sel_score_kernel spreads the scores of a tile over many workgroups and leaves
 // the keys in scratch for sel_pick_kernel.
 //
-// Measured, 32 query heads over 8, d_head 128: 32 of up to 512 blocks for 64 decoding steps 21 us (37 MB of signatures would be 8; lengths,
-// table, signatures, scores and choice wait for each other); 64 of 2048 blocks for each 16 of 2048 queries 57 us, of which the scores are 44:
+// Measured, 32 query heads over 8, d_head 128: 32 of up to 512 blocks for 64 decoding steps 19 us (37 MB of signatures would be 8; lengths,
+// table, signatures, scores and choice wait for each other); 64 of 2048 blocks for each 16 of 2048 queries 56 us, of which the scores are 44:
 // every workgroup reads all signatures of a head through L2, 268 MB in all; 64 of 2048 for one query 18 us.
 #include "attn.h"
 
@@ -29,6 +29,16 @@ struct SelectArgs {
 __device__ __forceinline__ unsigned order_key(float f) {         // larger float, larger key; never 0 or all ones for finite f
     const unsigned u = __float_as_uint(f + 0.0f);                // -0 counts as 0
     return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ float key_value(unsigned k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+
+// Where an interval of keys [lo, hi) is cut, hi - lo > 1: in the middle of the scores' values in even rounds (scores lie close
+// together there, so few rounds lead to the threshold), in the middle of the keys in odd ones (no more than 64 rounds, whatever the scores).
+__device__ __forceinline__ unsigned cut(unsigned lo, unsigned hi, int round) {
+    if (round & 1) return lo + (hi - lo) / 2;
+    const unsigned k = order_key(0.5f * key_value(lo) + 0.5f * key_value(hi));
+    return min(max(k, lo + 1), hi - 1);
 }
 
 // A tile's place in its sequence: its rows, and the blocks it may choose from.
@@ -110,8 +120,8 @@ __device__ __forceinline__ void pick_by_wave(unsigned* keys, int n, int lead, in
         } else {
             unsigned lo = ~s3_wave_max_u32(~least), hi = s3_wave_max_u32(most) + 1;      // more than `top` from lo on, at most that from hi on
             int from_lo = cand, from_hi = always;
-            while (hi - lo > 1 && from_lo - from_hi > 64) {
-                const unsigned mid = lo + (hi - lo) / 2;
+            for (int round = 0; hi - lo > 1 && from_lo - from_hi > 64; ++round) {
+                const unsigned mid = cut(lo, hi, round);
                 int c = 0;
                 for (int base = 0; base < n; base += 512) {
                     unsigned k[8];
@@ -261,7 +271,7 @@ __device__ __forceinline__ void pick_by_block(K key, int n, int top, PickScratch
             from_hi = 0;
         }
         while (hi - lo > 1 && from_lo - from_hi > 64 && always < top) {
-            const unsigned mid = lo + (hi - lo) / 2;
+            const unsigned mid = cut(lo, hi, round);
             const int c = count([&](unsigned x, int) { return x >= mid; });
             if (c > top) {
                 lo = mid;
@@ -412,6 +422,14 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 || WAVES == 4 ? 2 : 4) void se
     __syncthreads();
     const int fours = WHOLE ? p.qb * p.G / 4 : (min(p.qb, n) * p.G + 3) / 4;               // of a tile
     for (int f0 = 0; f0 < t_here * fours; f0 += NSETS * 8) {
+        // signatures are on their way before the rows are, and the next ones from the moment that a walk step's are used up
+        constexpr int K = D / 16;
+        auto lookup = [&](int blk) { return blk < nb ? kv_page(p.b, s, blk) : -1; };
+        auto sig_of = [&](int page) { return p.sig + ((int64_t)max(page, 0) * p.n_kv + head) * D + half * 8; };
+        kv_bf16x8 g[K];
+        int page = lookup(wave * 32 + col), next = lookup((wave + WAVES) * 32 + col);
+#pragma unroll
+        for (int k = 0; k < K; ++k) g[k] = *(const kv_bf16x8*)(sig_of(page) + k * 16);
         kv_bf16x8 a[NSETS][D / 16];
         auto rows_of = [&](int x) {
             const int f = f0 + x * 8 + (col >> 2), t = f / fours;
@@ -451,14 +469,6 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 || WAVES == 4 ? 2 : 4) void se
                 to[x][i] = tq < t_here ? tq * stride : -1;
             }
         }
-        // the next signatures are on their way from the moment that this walk step's are used up
-        constexpr int K = D / 16;
-        auto lookup = [&](int blk) { return blk < nb ? kv_page(p.b, s, blk) : -1; };
-        auto sig_of = [&](int page) { return p.sig + ((int64_t)max(page, 0) * p.n_kv + head) * D + half * 8; };
-        kv_bf16x8 g[K];
-        int page = lookup(wave * 32 + col), next = lookup((wave + WAVES) * 32 + col);
-#pragma unroll
-        for (int k = 0; k < K; ++k) g[k] = *(const kv_bf16x8*)(sig_of(page) + k * 16);
         for (int b = wave * 32; b < nb; b += WAVES * 32) {
             const int blk = b + col;
             const __bf16* sg = sig_of(next);
@@ -664,7 +674,7 @@ int launch_select(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
     if ((int64_t)grid.x * grid.y >= (int64_t)1 << 24 || grid.y > 65535) return s3_fail(S3_EINVAL, "s3_block_select: too many tiles in one call");
     hipLaunchKernelGGL((sel_score_kernel<T, D>), grid, dim3(kThreads), 0, st, p);
     S3_HIP(hipGetLastError());
-    // 8 tiles of 2048 / 15625 candidates, us a call: 21 / 86 with the first, 32 / 41 with the second
+    // 8 lists of 2048 / 15625 candidates, us a call: 21 / 86 with the first, 32 / 41 with the second
     if (p.nb <= 4096) hipLaunchKernelGGL(sel_pick_kernel, dim3(grid.x), dim3(kThreads), 0, st, p);
     else hipLaunchKernelGGL(sel_pick_long_kernel, dim3(grid.x), dim3(kPickWaves * 64), 0, st, p);
     S3_HIP(hipGetLastError());
