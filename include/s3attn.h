@@ -387,7 +387,7 @@ int s3_rope_table(float* table, int64_t n_pos, int rot_dim, double theta, void* 
  * in fp32 (partial sums over slots of equal remainder mod 8, in ascending order, then (0+1)+(2+3) and (4+5)+(6+7), joined, divided by the number),
  * rounded to whole multiples of 2^(floor(log2 max|m|) - 6): at most 128 of them, so bf16 holds it exactly.  Zero where max|m|
  * is not in [2^-40, 2^50).
- * Limits: n_q_heads a multiple of n_kv_heads where q is given. */
+ * Limits: n_q_heads a multiple of n_kv_heads, 32 times as many at most, where q is given. */
 int s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* k, int64_t k_tok_stride,
                  int64_t k_head_stride, const void* v, int64_t v_tok_stride, int64_t v_head_stride, const float* rope,
                  int64_t n_pos, int rot_dim, int interleaved, const int32_t* positions, const void* q, int n_q_heads,
@@ -418,7 +418,7 @@ int s3_paged_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const
  *   sel [s3_block_tiles(batch, q_block)][n_kv_heads][top_b] int32: the chosen blocks in ascending order, then -1 (tiles beyond the
  *       last one of the batch: all -1; s3_block_tiles is what n_tokens and n_seq allow).
  *   ws  s3_block_select_workspace(...) bytes, 256-byte aligned.
- * Limits: cache->sig; q_block >= 1; 1 <= top_b <= 4096; lead, tail >= 0; lead + tail + (q_block + page_size - 2) / page_size <= top_b. */
+ * Limits: cache->sig; n_q_heads as in s3_paged_attention; 1 <= q_block <= 2^20; 1 <= top_b <= 4096; lead, tail >= 0; lead + tail + (q_block + page_size - 2) / page_size <= top_b. */
 int64_t s3_block_tiles(const s3_kv_batch* batch, int q_block);
 size_t s3_block_select_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads, int q_block, int top_b);
 int s3_block_select(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,

@@ -41,7 +41,8 @@ struct Plan {
         G = n_q / c->n_kv_heads;
         limit = few_rows(c, q_block != 0);
         qb = min(q_block, max(b->n_tokens, 1));
-        const int64_t most = (int64_t)(q_block ? qb : min(max(b->max_new, 1), max(b->n_tokens, 1))) * G;
+        const int most_new = min(max(b->max_new, 1), max(b->n_tokens, 1));
+        const int64_t most = (int64_t)(q_block ? min(qb, most_new) : most_new) * G;
         many = most > limit;
         if (many && !q_block) limit = 32;                     // beside chunks the short ones are single tokens, mostly
         // no sequence is a short one if even the others at their longest leave more rows for it

@@ -395,6 +395,9 @@ def test_many_sequences_over_the_same_pages(new, G, n_seq, listed):
     ("fp32", 128, 16, 4, 2, [40, 1], [200, 90], 16, 6),
     ("fp32", 256, 32, 2, 1, [70], [200], 64, 5),
     ("bf16", 128, 256, 8, 2, [5], [1500], 5, 3),
+    ("bf16", 64, 16, 8, 2, [1, 1, 1], [90, 200, 7], 64, 5),            # tiles far larger than what a sequence brings
+    ("fp32", 128, 16, 8, 2, [20, 3], [90, 200], 32, 5),                # 80 rows a tile
+    ("bf16", 128, 16, 4, 1, [300], [400], 200, 9),                     # tiles of 800 rows
 ])
 def test_block_attention(dtype, d, P, hq, hkv, new, kv, qb, top):
     pr = paged.Problem(13 + d + qb, dtype, d, P, hq, hkv, new, kv, garbage=float("nan"))
