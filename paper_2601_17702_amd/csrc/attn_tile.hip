@@ -353,12 +353,12 @@ int s3_attn_tile_rows(const s3_kv_cache* c) { return rows_of(c); }
 // Into how many parts the tokens of a row tile are cut.  One workgroup fills a compute unit, so units tiles * heads take
 // ceil(units / 256) turns of all their steps; parts make the last turn fuller, at the price of writing fp32 sums and joining them.
 // In us, with the rates that the kernel reaches on a compute unit: 3.8 TFLOP/s in bf16 and 0.45 in fp32, 6 us for the joining
-// kernel and a tile's sums at 20 GB/s.
+// kernel, a part's sums written and read at 20 GB/s, and 4 us for its beginning.
 int s3_attn_tile_split(const s3_kv_cache* c, int64_t units, int64_t tokens) {
     const bool bf = c->dtype == S3_BF16;
     const int kt = c->d_head * (bf ? 2 : 4) > 512 ? 32 : 64;
     const int64_t steps = (tokens + kt - 1) / kt;
-    const double step = 4.0 * rows_of(c) * kt * c->d_head / (bf ? 3.8e6 : 0.45e6), sums = rows_of(c) * (c->d_head + 2) * 4 / 20e3;
+    const double step = 4.0 * rows_of(c) * kt * c->d_head / (bf ? 3.8e6 : 0.45e6), sums = rows_of(c) * (c->d_head + 2) * 4 / 10e3 + 4.0;
     int best = 1;
     double least = 1e30;
     for (int n = 1; n <= 64 && n <= steps; ++n) {
