@@ -55,16 +55,17 @@ struct Plan {
         const int rows = s3_attn_tile_rows(c);
         per_q = !q_block ? 1 : (int)((most + (many ? rows : tile) - 1) / (many ? rows : tile));
         few_tiles = q_block ? s3_block_tiles(b, q_block) * per_q : min(((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * (tile - 1)) / tile, (int64_t)b->n_seq);
-        many_tiles = !many ? 0 : q_block ? s3_block_tiles(b, q_block) * per_q
-                                         : ((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * (rows - 1)) / rows;
+        // row tiles that there can be: beside the streaming kernel only sequences of more than `limit` rows have any, and each ends in one
+        // that is not full; none has more than max_new tokens
+        const int64_t all = (int64_t)b->n_tokens * G, longs = min((int64_t)min(b->n_seq, b->n_tokens), few ? all / (limit + 1) : all);
+        many_tiles = !many ? 0 : q_block ? s3_block_tiles(b, q_block) * per_q : min((all + longs * (rows - 1)) / rows, longs * ((most + rows - 1) / rows));
         const int64_t units = many_tiles * c->n_kv_heads, tokens = q_block ? (int64_t)top_b * c->page_size : b->max_kv;
-        // a chunk beside a few short ones: its row tiles decide, the others fill what it leaves idle (2048, 275 and 37 tokens of 28 heads over 4:
-        // 1054 us cut in two for 268 tiles, 991 whole for the 224 of the longest)
-        const int64_t longest = (int64_t)min(b->max_new, b->n_tokens) * G, share = (longest + rows - 1) / rows * c->n_kv_heads;
-        const int64_t weigh = !q_block && ((int64_t)b->n_tokens * G - longest) * 6 <= longest ? share : units;
-        n_split = many ? s3_attn_tile_split(c, weigh, tokens) : 1;
+        // Every tile that there can be weighs the same, for the host knows no sequence's own length.  Weighed by the longest chunk's tiles alone, 2048 tokens
+        // at 2048 beside eight times 30 at 131072 took 2546 us instead of 1293 (the short ones' tiles see most), 256 at 131072 beside 42 single
+        // tokens 791 instead of 1027.
+        n_split = many ? s3_attn_tile_split(c, units, tokens) : 1;
         many_ws = s3_attn_tile_workspace(c, units, n_split);              // for any window
-        if (many && window) n_split = min(n_split, s3_attn_tile_split(c, weigh, min(tokens, (int64_t)window + rows / G)));
+        if (many && window) n_split = min(n_split, s3_attn_tile_split(c, units, min(tokens, (int64_t)window + rows / G)));
     }
 };
 

@@ -1,0 +1,31 @@
+"""CPU-only checks of how much scratch the paged cache's calls ask for (heads of 128 channels in bf16 unless said)."""
+import pytest
+
+import paper_2601_17702_amd as s3
+from tests.test_paged_args import batch, cache
+
+
+def scratch(n_seq, n_tokens, max_new, max_kv, n_q=32, heads=8, d=128, dtype=0):
+    c = cache(n_pages=1 << 20, heads=heads, d=d, dtype=dtype)
+    pages = -(-max_kv // 64)
+    return s3.lib().s3_paged_attention_workspace(c, batch(n_seq=n_seq, n_tokens=n_tokens, max_pages=pages, stride=pages, max_new=max_new, max_kv=max_kv), n_q)
+
+
+@pytest.mark.parametrize("n_seq,n_tokens,max_new,max_kv,n_q,heads", [
+    (64, 64, 64, 32768, 32, 8),              # single tokens with starts, the bound of a sequence's new tokens left at its default
+    (256, 256, 256, 32768, 32, 8),
+    (16, 16, 16, 131072, 32, 8),
+    (43, 298, 256, 131072, 8, 8),            # one chunk beside single tokens
+    (9, 2048 + 240, 2048, 131072, 32, 8),    # a long chunk beside short turns
+    (64, 4096, 4096, 32768, 28, 4),
+])
+def test_scratch_of_parts_is_bounded(n_seq, n_tokens, max_new, max_kv, n_q, heads):
+    """Parts are cut until some 2048 workgroups are there, whatever the bounds of a call say, and only for row tiles that can be there: a part of 256
+    rows holds 256 * 130 floats, so 2048 of them 273 MB; the streaming kernel's two per workgroup 34 MB at most beside that."""
+    assert scratch(n_seq, n_tokens, max_new, max_kv, n_q, heads) <= 2048 * 256 * 130 * 4 + 1024 * 32 * 130 * 4
+
+
+def test_scratch_of_a_decoding_batch_without_a_bound():
+    """64 single tokens of which the host says only that there are 64: at most 7 sequences can have the 33 rows that make a chunk."""
+    assert scratch(64, 64, 64, 32768) <= 128 << 20
+    assert scratch(64, 64, 1, 32768) <= 4 << 20
