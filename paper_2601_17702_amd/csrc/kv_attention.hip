@@ -93,6 +93,7 @@ extern "C" int s3_paged_attention(const s3_kv_cache* c, const s3_kv_batch* b, co
     const char* fn = "s3_paged_attention";
     if (window < 0) return s3_fail(S3_EINVAL, "%s: window %d", fn, window);
     if (int rc = check(fn, c, b, q, n_q, q_ts, q_hs, scale, out)) return rc < 0 ? rc : S3_OK;
+    if (window >= 1 << 30) window = 0;                        // no position is that far back: all of them, and none of the kernels' differences overflows
     const Plan plan(c, b, n_q, 0, 0, window);
     if (int rc = check_ws(fn, ws, ws_bytes, plan.bytes())) return rc;
     const int es = c->dtype == S3_BF16 ? 2 : 4;
