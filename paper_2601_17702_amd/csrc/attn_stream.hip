@@ -26,6 +26,9 @@ __device__ __forceinline__ int64_t wave_incl_scan64(int64_t x) {
     return x;
 }
 
+// fp32 of a scratch slot: R rows' sums, their maxima and the weights' sums; whole 16-byte pieces, for R may be odd.
+__host__ __device__ __forceinline__ int64_t slot_floats(int R, int D) { return ((int64_t)R * (D + 2) + 3) & ~(int64_t)3; }
+
 // A sequence's part of the line: tiles of rows, each with n_kv heads of `pieces` pieces that begin at token lo.
 struct Part {
     int first, n, len, lo, tiles, pieces;
@@ -314,7 +317,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         }
         __syncthreads();
         const bool whole = c0 == 0 && c1 == part.pieces;
-        float* slot = slots + ((int64_t)blockIdx.x * 2 + (c0 == 0)) * ((int64_t)R * (D + 2));
+        float* slot = slots + ((int64_t)blockIdx.x * 2 + (c0 == 0)) * slot_floats(R, D);
         const int n_rows = min(R, r_end - r0);
         for (int i = tid; i < n_rows * (D / 4); i += kThreads) {
             const int r = i / (D / 4), c = i % (D / 4) * 4, first = r / 32, rr = r & 31;
@@ -390,7 +393,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const f
     int r0, r_end;
     rows_of<LIST, RT>(p, part, (int)want, r0, r_end);
     const int n_rows = min(R, r_end - r0);
-    const int64_t stride = (int64_t)R * (D + 2);
+    const int64_t stride = slot_floats(R, D);
     const int k = tid >> 5;
     constexpr int kShare = kThreads / 32;
     for (int x = blockIdx.y; x < (n_rows + 3) / 4 * (D / 32); x += gridDim.y) {
@@ -449,7 +452,7 @@ int launch(const AttnArgs& p, int64_t tiles, int R, float* ws, hipStream_t st) {
 
 }  // namespace
 
-size_t s3_attn_stream_workspace(int d_head, int R) { return s3_align((size_t)kRunGroups * 2 * R * (d_head + 2) * 4); }
+size_t s3_attn_stream_workspace(int d_head, int R) { return s3_align((size_t)kRunGroups * 2 * slot_floats(R, d_head) * 4); }
 
 int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st) {
     const int rt = R <= 32 ? 1 : R <= 64 ? 2 : 4;

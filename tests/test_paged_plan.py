@@ -29,3 +29,11 @@ def test_scratch_of_a_decoding_batch_without_a_bound():
     """64 single tokens of which the host says only that there are 64: at most 7 sequences can have the 33 rows that make a chunk."""
     assert scratch(64, 64, 64, 32768) <= 128 << 20
     assert scratch(64, 64, 1, 32768) <= 4 << 20
+
+
+@pytest.mark.parametrize("G", [1, 3, 7, 8])
+@pytest.mark.parametrize("d,dtype", [(64, 0), (128, 0), (256, 1)])
+def test_slots_of_the_streaming_kernel_are_whole_pieces(G, d, dtype):
+    """512 workgroups have two slots each, which are written and read 16 bytes at a time, for odd numbers of rows, too."""
+    slot, rest = divmod(scratch(4, 4, 1, 4096, 2 * G, 2, d, dtype), 1024)
+    assert rest == 0 and slot % 16 == 0 and slot >= G * (d + 2) * 4
