@@ -397,8 +397,8 @@ int s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const void*
  *   out[t, h] = sum_j softmax_j(scale q[t, h] . k[j, h / G]) v[j, h / G] over the positions j <= p (t's own), and
  *   j > p - window where window > 0; G = n_q_heads / n_kv_heads.
  *   lse[t, h] = log sum_j exp(scale q . k) (natural log), or NULL.
- * A row that sees nothing (kv_len smaller than the number of new tokens, unmapped pages) is 0 with lse -inf.  Values in masked
- * places never reach a row, infinities and NaN included.
+ * A row that sees nothing (kv_len smaller than the number of new tokens, unmapped pages) is 0 with lse -inf; one that sees tokens, but
+ * scores of -inf only, is NaN with lse -inf.  Values in masked places never reach a row, infinities and NaN included.
  * Softmax statistics and sums in fp32; with bf16 the weights are rounded to bf16 for the second product.
  *   q    [n_tokens][n_q_heads][d_head], strides as in s3_kv_append;  out [n_tokens][n_q_heads][d_head] contiguous, dtype
  *   ws   s3_paged_attention_workspace(...) bytes, 256-byte aligned, contents meaningless between calls

@@ -133,10 +133,10 @@ struct AttnSight {
 };
 
 // Running softmax of a row: m the scaled score (log2 units) that its weights are taken against, at most kSlack below the largest so
-// far; l this lane's part of the weights' sum, o the products so far: o[dt][i] is channel 32 dt + 8 (i / 4) + 4 half + i % 4.
+// far, -inf before there is one; l this lane's part of the weights' sum, o the products so far: o[dt][i] is channel 32 dt + 8 (i / 4) + 4 half + i % 4.
 // Rescaling o takes D / 2 instructions per 32 tokens, more than the exponentials: it is done only where a row's largest score has
 // grown by more than kSlack (weights of up to 2^kSlack are as exact as those below 1).
-constexpr float kSlack = 8.0f;
+constexpr float kSlack = 8.0f, kLowest = -3.402823466e38f;
 template <typename T, int D>
 struct AttnState {
     typedef typename KvElem<T>::vec vec;
@@ -166,6 +166,13 @@ struct AttnState {
         }
         return m == -INFINITY ? 0.0f : m;                       // nothing seen yet: every weight is exp2(-inf)
     }
+    // Behind the last scores: a row that saw tokens, but scores of -inf only, has no weights and is NaN; m tells it from one that saw
+    // nothing and is 0.  seen: the lane had a token that the row sees.
+    __device__ __forceinline__ void settle(bool seen) {
+        const unsigned any = seen ? 1u : 0u;
+        const auto r = __builtin_amdgcn_permlane32_swap(any, any, false, false);
+        if ((r[0] | r[1]) != 0 && m == -INFINITY) m = kLowest;
+    }
     // Weights of E of the lane's 16 tokens: registers E y .. of raw scores, -inf where masked.
     __device__ __forceinline__ vec weights(const kv_f32x16& s, int y, float sl, float sub) {
         vec w;
@@ -194,8 +201,8 @@ struct AttnState {
     }
 };
 
-// 1 / l, or what makes a row that saw nothing 0; its lse.
-__device__ __forceinline__ float kv_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+// 1 / l, or what makes a row that saw nothing 0 (infinity makes NaN of one that saw only scores of -inf); its lse.
+__device__ __forceinline__ float kv_inverse(float m, float l) { return m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l; }
 __device__ __forceinline__ float kv_lse(float m, float l) { return l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f; }
 // What brings sums against m (l the weights' sum) to sums against the larger m2; sums of nothing count as zero.
 __device__ __forceinline__ float kv_factor(float m, float l, float m2) {

@@ -150,6 +150,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         rows.load(p, head, part.first, part.n, part.len, r0 + set * 32 + col, r_end);
         AttnState<T, D> st;
         st.clear();
+        bool seen = false;
         const int pos0 = part.len - part.n + (r0 + set * 32) / p.G;               // the set's first row's position
         const int last = part.len - part.n + (r_end - 1) / p.G;                   // the last row's; its tokens end at hi
         const int hi = min(last + 1, kv_blocks(p.b, part.len) << logp);
@@ -239,8 +240,12 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
                         const int t = 2 * E * (x / E) + E * half + x % E;
-                        sc[0][x] = sight.sees((2 * E * (x / E) < 16 ? a.x : b.x) + (t & 15)) ? sc[0][x] : -INFINITY;
+                        const bool sees = sight.sees((2 * E * (x / E) < 16 ? a.x : b.x) + (t & 15));
+                        seen |= sees;
+                        sc[0][x] = sees ? sc[0][x] : -INFINITY;
                     }
+                } else {
+                    seen = true;
                 }
                 float x = sc[0][0];
 #pragma unroll
@@ -295,6 +300,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         }
 
         // the sums of a row set's wavefronts
+        st.settle(seen);
         const float l = kv_pair_sum(st.l);
         if (half == 0) {
             sum_m[wave * 32 + col] = st.m;
@@ -334,7 +340,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
             if (whole) {
                 const int t = (r0 + r) / p.G;
                 const int64_t row = (int64_t)(part.first + t) * p.n_q + head * p.G + (r0 + r - t * p.G);
-                const float inv = kv_inverse(lsum);
+                const float inv = kv_inverse(m, lsum);
                 typedef __attribute__((ext_vector_type(4))) T four;
                 *(four*)(p.out + (row * D + c) * ES) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
                 if (p.lse && c == 0) p.lse[row] = kv_lse(m, lsum);
@@ -427,7 +433,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs p, const f
             }
             const int t = (r0 + r) / p.G;
             const int64_t row = (int64_t)(part.first + t) * p.n_q + head * p.G + (r0 + r - t * p.G);
-            const float inv = kv_inverse(l);
+            const float inv = kv_inverse(m, l);
             typedef __attribute__((ext_vector_type(4))) T four;
             *(four*)(p.out + (row * D + c) * (int)sizeof(T)) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
             if (p.lse && c == 0) p.lse[row] = kv_lse(m, l);

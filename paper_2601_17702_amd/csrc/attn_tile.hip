@@ -69,6 +69,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
     AttnState<T, D> st;
     rows.load(p, head, first, n, len, rw + col, r_end);
     st.clear();
+    bool seen = false;
     const AttnSight sight(rows.pos, hi, p.window);
 
     // what some row of the workgroup does not see: such steps are masked, and their values looked at
@@ -206,8 +207,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int tk = x * 32 + 2 * E * (i / E) + E * half + i % E;
-                            sc[x][i] = sight.sees(runs[t * (KT / 16) + (x * 32 + 2 * E * (i / E)) / 16].w + (tk & 15)) ? sc[x][i] : -INFINITY;
+                            const bool sees = sight.sees(runs[t * (KT / 16) + (x * 32 + 2 * E * (i / E)) / 16].w + (tk & 15));
+                            seen |= sees;
+                            sc[x][i] = sees ? sc[x][i] : -INFINITY;
                         }
+                } else {
+                    seen = true;
                 }
                 float top = sc[0][0];
 #pragma unroll
@@ -251,6 +256,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
         }
     }
 
+    st.settle(seen);
     const float l = kv_pair_sum(st.l);
     if (ta.n_split > 1) {
         const int row = wave * 32 + col;
@@ -268,7 +274,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void attn_tile_kernel(AttnAr
             }
         }
     } else if (rows.row >= 0) {
-        const float inv = kv_inverse(l);
+        const float inv = kv_inverse(st.m, l);
         char* out = p.out + rows.row * (D * ES);
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
@@ -316,7 +322,7 @@ __global__ __launch_bounds__(256) void attn_tile_join_kernel(AttnArgs p, TileArg
         }
         const int t = (r0 + row) / p.G;
         const int64_t at = (int64_t)(first + t) * p.n_q + head * p.G + (r0 + row - t * p.G);
-        const float inv = kv_inverse(l);
+        const float inv = kv_inverse(m, l);
         typedef __attribute__((ext_vector_type(4))) T four;
         *(four*)(p.out + (at * D + c) * (int)sizeof(T)) = four{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
         if (p.lse && c == 0) p.lse[at] = kv_lse(m, l);

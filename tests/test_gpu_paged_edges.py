@@ -28,3 +28,37 @@ def test_an_odd_number_of_rows_in_parts(dtype, d, hq, hkv):
     kv_len, table = pr.args()
     o, lse = pr.cache().attention(pr.q.cuda(), kv_len, table, want_lse=True)
     paged.check(pr, o, lse, paged.attend(pr))
+
+
+@pytest.mark.parametrize("listed", [False, True])
+@pytest.mark.parametrize("dtype,d,hq,new,kv,blocks", [
+    ("bf16", 64, 4, [1, 1], [96, 4000], [3, 60]),         # one token that sees nothing else; the first of a workgroup's tokens, and whole workgroups'
+    ("bf16", 128, 8, [150], [150], [2]),                  # a prompt: its first rows see nothing else
+    ("bf16", 256, 4, [40, 5], [70, 64], [1, 2]),
+    ("fp32", 64, 4, [70, 2], [2000, 64], [40, 2]),        # row tiles in parts
+    ("fp32", 128, 4, [3, 100], [31, 200], [1, 4]),
+    ("fp32", 256, 2, [90], [120], [2]),
+])
+def test_rows_that_see_scores_of_minus_infinity_only(dtype, d, hq, new, kv, blocks, listed):
+    """The softmax of such a row is 0 / 0: NaN with lse -inf, not the zeros of a row that sees nothing.  Rows that see a finite score
+    too are as if the others were not there.  An infinite key against queries of the other sign, in the first blocks of every sequence."""
+    P = 32
+    pr = paged.Problem(21 + d, dtype, d, P, hq, 2, new, kv, garbage=float("nan"))
+    pr.q[..., 0] = -pr.q[..., 0].abs() - 1
+    for rows, n in zip(pr.rows_k, blocks):
+        rows[:n * P, :, 0] = float("inf")
+    kv_len, table = pr.args()
+    c, q, qs = pr.cache(), pr.q.cuda(), pr.q_start.cuda()
+    for s, n in enumerate(blocks):
+        pr.table[s, :n] = -1                                            # for the reference they are not there
+    want, l64, tol, ltol = paged.attend(pr)
+    if listed:
+        sel = torch.arange(table.shape[1], dtype=torch.int32, device="cuda").repeat(pr.tiles(16), 2, 1).contiguous()
+        o, lse = c.block_attention(q, kv_len, table, sel, q_start=qs, q_block=16, want_lse=True)
+    else:
+        o, lse = c.attention(q, kv_len, table, q_start=qs, max_new=max(new), max_kv=max(kv), want_lse=True)
+    o, lse = o.cpu().to(torch.float64), lse.cpu().to(torch.float64)
+    none = torch.isinf(l64)
+    assert none.any()
+    assert torch.isnan(o[none]).all() and torch.all(lse[none] == -float("inf"))
+    assert torch.all((o - want).abs()[~none] <= tol[~none]) and torch.all((lse - l64).abs()[~none] <= ltol[~none])
