@@ -359,7 +359,9 @@ typedef struct {
  * Host structs of device pointers; the arrays are read when the kernels run.  What they hold cannot be checked on
  * the host: tokens past n_tokens are left out, a position whose block is beyond max_pages or whose page number is outside
  * [0, n_pages) is not stored and is masked for every reader, and rows of no sequence are not written.
- * Limits: n_seq <= 2^20, n_tokens <= 2^24, max_pages * page_size <= 2^30, kv_len <= 2^30; n_tokens == 0 is a no-op. */
+ * Limits: n_seq <= 2^20, n_tokens <= 2^24, max_pages <= table_stride, max_pages * page_size <= 2^30, kv_len <= 2^30; n_tokens == 0 is a no-op
+ * (s3_block_select then writes its lists: -1).  A call's workgroups each read all n_seq lengths, and each call names how much one launch
+ * takes: beyond either, cut the batch. */
 typedef struct {
     const int32_t* q_start;
     const int32_t* kv_len;
@@ -370,7 +372,7 @@ typedef struct {
 
 /* cos | sin of the rotary embedding, rounded once from 64 bits: table[p][i] = cos(a), table[p][rot_dim / 2 + i] = sin(a) with
  * a = p * theta^(-2 i / rot_dim), i < rot_dim / 2.  table [n_pos][rot_dim] fp32, 16-byte aligned.  rot_dim a multiple of 16, <= 256;
- * n_pos >= 0; theta > 0. */
+ * 0 <= n_pos <= 2^30, n_pos * rot_dim < 2^33 - 512; theta > 0. */
 int s3_rope_table(float* table, int64_t n_pos, int rot_dim, double theta, void* stream);
 
 /* Appends the batch's tokens: keys and values go to their slots, keys rotated on the way, the queries of the same
@@ -387,7 +389,8 @@ int s3_rope_table(float* table, int64_t n_pos, int rot_dim, double theta, void* 
  * in fp32 (partial sums over slots of equal remainder mod 8, in ascending order, then (0+1)+(2+3) and (4+5)+(6+7), joined, divided by the number),
  * rounded to whole multiples of 2^(floor(log2 max|m|) - 6): at most 128 of them, so bf16 holds it exactly.  Zero where max|m|
  * is not in [2^-40, 2^50).
- * Limits: n_q_heads a multiple of n_kv_heads, 32 times as many at most, where q is given. */
+ * Limits: n_q_heads a multiple of n_kv_heads, 32 times as many at most, where q is given.  Pages times n_kv_heads below 2^24, a quarter of
+ * n_tokens counted with them where q is given; pages are n_seq without q_start, n_seq + (n_tokens + n_seq (page_size - 2)) / page_size with it. */
 int s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* k, int64_t k_tok_stride,
                  int64_t k_head_stride, const void* v, int64_t v_tok_stride, int64_t v_head_stride, const float* rope,
                  int64_t n_pos, int rot_dim, int interleaved, const int32_t* positions, const void* q, int n_q_heads,
@@ -402,7 +405,8 @@ int s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const void*
  * Softmax statistics and sums in fp32; with bf16 the weights are rounded to bf16 for the second product.
  *   q    [n_tokens][n_q_heads][d_head], strides as in s3_kv_append;  out [n_tokens][n_q_heads][d_head] contiguous, dtype
  *   ws   s3_paged_attention_workspace(...) bytes, 256-byte aligned, contents meaningless between calls
- * Limits: 1 <= G <= 32; scale > 0; window >= 0. */
+ * Limits: 1 <= G <= 32; scale > 0; window >= 0.  n_kv_heads times n_seq below 2^22, and times the chunks' tiles of 128 rows (n_tokens * G / 128,
+ * one more for every sequence of more than 32 rows). */
 size_t s3_paged_attention_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads);
 int s3_paged_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
                        int64_t q_tok_stride, int64_t q_head_stride, float scale, int window, void* out, float* lse,
@@ -418,7 +422,9 @@ int s3_paged_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const
  *   sel [s3_block_tiles(batch, q_block)][n_kv_heads][top_b] int32: the chosen blocks in ascending order, then -1 (tiles beyond the
  *       last one of the batch: all -1; s3_block_tiles is what n_tokens and n_seq allow).
  *   ws  s3_block_select_workspace(...) bytes, 256-byte aligned.
- * Limits: cache->sig; n_q_heads as in s3_paged_attention; 1 <= q_block <= 2^20; 1 <= top_b <= 4096; lead, tail >= 0; lead + tail + (q_block + page_size - 2) / page_size <= top_b. */
+ * Limits: cache->sig; n_q_heads as in s3_paged_attention; 1 <= q_block <= 2^20; 1 <= top_b <= 4096; 0 <= lead <= top_b; tail >= 0, and with tail > 0
+ * lead + tail + (q_block + page_size - 2) / page_size <= top_b.  Lists (tiles * n_kv_heads) below 2^23; where max_kv spans more than 30720 blocks, lists *
+ * blocks below 2^31 - 2^24 and blocks below 2^23 - 128. */
 int64_t s3_block_tiles(const s3_kv_batch* batch, int q_block);
 size_t s3_block_select_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads, int q_block, int top_b);
 int s3_block_select(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
@@ -427,7 +433,8 @@ int s3_block_select(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
 
 /* s3_paged_attention over the positions of listed blocks only: sel as s3_block_select writes it, or made from the
  * spans of s3_coactivate_score / s3_select_spans.  Entries that are negative, beyond the sequence or unmapped are passed over, in any
- * place; a block listed twice counts twice.  The causal limit holds inside the listed blocks. */
+ * place; a block listed twice counts twice.  The causal limit holds inside the listed blocks.
+ * Limits: as s3_paged_attention; 1 <= q_block <= 2^20; 1 <= top_b <= 4096; lists below 2^22, a tile of more than 128 rows counted once for every 128. */
 size_t s3_block_attention_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads, int q_block, int top_b);
 int s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
                        int64_t q_tok_stride, int64_t q_head_stride, const int32_t* sel, int q_block, int top_b,

@@ -1,8 +1,8 @@
-// What the attention's entry points call (host).
+// What the attention's entry points call (host), with fewer than 2^22 tiles times heads.
 #pragma once
 #include "attn.h"
 
-// Sequences, or tiles of listed blocks, of at most 32 rows (R: the most that one has, 128 at most); tiles: how many there can be.
+// Sequences, or tiles of listed blocks, of few rows (R: the most that one has, 128 at most); tiles: how many there can be.
 size_t s3_attn_stream_workspace(int d_head, int R);
 int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
 

@@ -448,7 +448,6 @@ int launch(const AttnArgs& p, int64_t tiles, int R, float* ws, hipStream_t st) {
     const int bytes = kWaves * 32 * 8 + (kBatchRuns + 16) * 8 + kWaves * min(R, 32) * (D + 4) * 4;
     if (int rc = s3_allow_lds(once, (const void*)attn_stream_kernel<T, D, LIST, RT>, kWaves * 32 * 8 + (kBatchRuns + 16) * 8 + kWaves * 32 * (D + 4) * 4)) return rc;
     const int64_t join = tiles * p.n_kv;
-    if (join >= (int64_t)1 << 22) return s3_fail(S3_EINVAL, "attention: too many tokens in one call");
     hipLaunchKernelGGL((attn_stream_kernel<T, D, LIST, RT>), dim3(kRunGroups), dim3(kThreads), bytes, st, p, ws, R);
     S3_HIP(hipGetLastError());
     hipLaunchKernelGGL((attn_join_kernel<T, D, LIST, RT>), dim3((unsigned)join, (unsigned)max((int64_t)1, min(4096 / join, (int64_t)(D / 32 * ((R + 3) / 4))))), dim3(kThreads), 0, st, p, ws, R, kRunGroups);

@@ -342,7 +342,6 @@ int launch(const AttnArgs& p, const TileArgs& ta, hipStream_t st) {
     static S3LdsOnce once;
     if (int rc = s3_allow_lds(once, (const void*)attn_tile_kernel<T, D, LIST, W>, bytes)) return rc;
     const int64_t units = (int64_t)ta.tiles * p.n_kv;
-    if (units >= (int64_t)1 << 22) return s3_fail(S3_EINVAL, "attention: too many tokens in one call");
     hipLaunchKernelGGL((attn_tile_kernel<T, D, LIST, W>), dim3((unsigned)units, ta.n_split), dim3(W * 64), bytes, st, p, ta);
     S3_HIP(hipGetLastError());
     if (ta.n_split > 1) {
@@ -384,7 +383,6 @@ size_t s3_attn_tile_workspace(const s3_kv_cache* c, int64_t units, int n_split) 
 }
 
 int s3_attn_tile(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int n_split, void* ws, hipStream_t st) {
-    if (tiles * p.n_kv >= (int64_t)1 << 22) return s3_fail(S3_EINVAL, "attention: too many tokens in one call");
     const TileArgs ta{(float*)ws, n_split, (int)tiles};
 #define S3_TILE(T, D) (p.sel ? launch<T, D, true>(p, ta, st) : launch<T, D, false>(p, ta, st))
     if (c->dtype == S3_BF16) return c->d_head == 64 ? S3_TILE(__bf16, 64) : c->d_head == 128 ? S3_TILE(__bf16, 128) : S3_TILE(__bf16, 256);

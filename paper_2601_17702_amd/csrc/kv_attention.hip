@@ -73,6 +73,9 @@ int run(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b, AttnArgs p, 
     p.few = plan.few ? plan.limit : 0;
     p.qb = plan.qb;
     p.per_q = plan.per_q;
+    // the joins' grids; looked at before the first launch, so that a refused call has written nothing
+    if (max(plan.few ? plan.few_tiles : 0, plan.many_tiles) * c->n_kv_heads >= (int64_t)1 << 22)
+        return s3_fail(S3_EINVAL, "%s: %lld row tiles and %d heads are too many for one call", fn, (long long)max(plan.few_tiles, plan.many_tiles), c->n_kv_heads);
     if (plan.few)
         if (int rc = s3_attn_stream(c, p, plan.few_tiles, plan.R, ws, st)) return rc;
     return plan.many ? s3_attn_tile(c, p, plan.many_tiles, plan.n_split, (char*)ws + plan.few_ws, st) : S3_OK;

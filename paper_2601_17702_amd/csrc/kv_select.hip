@@ -671,7 +671,6 @@ int launch_select(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
         return plan.whole ? launch_fused<T, D, 2, 4, true>(p, plan, st) : launch_fused<T, D, 2, 4, false>(p, plan, st);
     }
     const dim3 grid((unsigned)(plan.tiles * p.n_kv), (unsigned)((p.nb + kScoreBlocks - 1) / kScoreBlocks));
-    if ((int64_t)grid.x * grid.y >= (int64_t)1 << 24 || grid.y > 65535) return s3_fail(S3_EINVAL, "s3_block_select: too many tiles in one call");
     hipLaunchKernelGGL((sel_score_kernel<T, D>), grid, dim3(kThreads), 0, st, p);
     S3_HIP(hipGetLastError());
     // 8 lists of 2048 / 15625 candidates, us a call: 21 / 86 with the first, 32 / 41 with the second
@@ -709,7 +708,10 @@ extern "C" int s3_block_select(const s3_kv_cache* c, const s3_kv_batch* b, const
     const size_t need = plan.workspace(c->n_kv_heads);
     if (need && (!ws || (uintptr_t)ws & 255)) return s3_fail(S3_EINVAL, "%s: workspace is null or not 256-byte aligned", fn);
     if (ws_bytes < need) return s3_fail(S3_ECAPACITY, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
-    if (tiles * c->n_kv_heads >= (int64_t)1 << 24) return s3_fail(S3_EINVAL, "%s: too many tiles in one call", fn);
+    // a launch has fewer than 2^32 threads: 512 a list, or 256 for every 128 candidates of one
+    const int64_t lists = tiles * c->n_kv_heads, parts = (plan.nb + kScoreBlocks - 1) / kScoreBlocks;
+    if (lists >= (int64_t)1 << 23 || (!plan.fused && (lists * parts >= (int64_t)1 << 24 || parts > 65535)))
+        return s3_fail(S3_EINVAL, "%s: %lld lists over %d blocks are too many for one call", fn, (long long)lists, plan.nb);
     const int es = c->dtype == S3_BF16 ? 2 : 4;
     SelectArgs p{s3_kv_batch_args(c, b), (const char*)q, q_ts * es, q_hs * es, (const __bf16*)c->sig, (unsigned*)ws, sel,
                  c->n_kv_heads, n_q / c->n_kv_heads, q_block, top_b, lead, tail, plan.nb};

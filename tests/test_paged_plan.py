@@ -37,3 +37,25 @@ def test_slots_of_the_streaming_kernel_are_whole_pieces(G, d, dtype):
     """512 workgroups have two slots each, which are written and read 16 bytes at a time, for odd numbers of rows, too."""
     slot, rest = divmod(scratch(4, 4, 1, 4096, 2 * G, 2, d, dtype), 1024)
     assert rest == 0 and slot % 16 == 0 and slot >= G * (d + 2) * 4
+
+
+def attend(b, heads, G=1):
+    return s3.lib().s3_paged_attention(cache(heads=heads), b, 4096, heads * G, 1 << 20, 128, 0.1, 0, 4096, None, 4096, 1 << 50, None)
+
+
+def test_calls_too_large_for_one_launch_are_refused_before_any():
+    """S3_EINVAL on the host, with nothing launched (where there is no GPU a launch gives S3_EHIP)."""
+    wide = dict(max_pages=16, stride=16, max_kv=1024)
+    # 2^20 single tokens of 8 heads: a join of 2^23 workgroups
+    assert attend(batch(qs=0, n_seq=1 << 20, n_tokens=1 << 20, max_new=1, **wide), 8) == -1
+    # short turns are few, but not the tiles of the chunks beside them: the kernel of the short ones is not launched either
+    assert attend(batch(n_seq=3, n_tokens=300000, max_new=150000, **wide), 4096) == -1
+    assert b"too many" in s3.lib().s3_last_error()
+    def choose(n_tokens, heads, max_kv, page=16):
+        pages = -(-max_kv // page)
+        b = batch(n_seq=1, n_tokens=n_tokens, max_new=n_tokens, max_pages=pages, stride=pages, max_kv=max_kv)
+        return s3.lib().s3_block_select(cache(page=page, heads=heads), b, 4096, heads * 32, 1 << 20, 128, 1, 16, 1, 1, 4096, 4096, 1 << 50, None)
+    # 2^23 lists of 512 threads are 2^32 threads
+    assert choose(1 << 13, 1 << 10, 1024) == -1
+    assert b"too many" in s3.lib().s3_last_error()
+    assert choose(1 << 15, 8, 1 << 20) == -1 and choose(1, 1, 1 << 30) == -1
