@@ -564,6 +564,13 @@ class KVCache:
             _check(rc)
         return q_out
 
+    @staticmethod
+    def _scratch(q, need, ws):
+        if ws is None:
+            return q.new_empty(need, dtype=_torch().uint8) if need else None
+        assert ws.is_cuda and ws.is_contiguous()
+        return ws
+
     def _out(self, q, out, want_lse, need, ws):
         torch = _torch()
         if out is None:
@@ -571,9 +578,7 @@ class KVCache:
         else:
             assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.is_cuda
         lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
-        if ws is None and need:
-            ws = q.new_empty(need, dtype=torch.uint8)
-        return out, lse, ws
+        return out, lse, self._scratch(q, need, ws)
 
     def attention(self, q, kv_len, block_table, q_start=None, scale=None, window: int = 0, max_new=None, max_kv=None, out=None,
                   want_lse: bool = False, ws=None):
@@ -600,8 +605,7 @@ class KVCache:
         qp, qt, qh = self._rows(q)
         sel = q.new_empty((_lib.s3_block_tiles(b, q_block), self.n_kv_heads, top_b), dtype=torch.int32)
         need = _lib.s3_block_select_workspace(self._c, b, n_q, q_block, top_b)
-        if ws is None and need:
-            ws = q.new_empty(need, dtype=torch.uint8)
+        ws = self._scratch(q, need, ws)
         rc = _lib.s3_block_select(self._c, b, qp, n_q, qt, qh, q_block, top_b, lead, tail, sel.data_ptr(), _ptr(ws),
                                   0 if ws is None else ws.numel(), _stream())
         if rc:

@@ -62,3 +62,18 @@ def test_rows_that_see_scores_of_minus_infinity_only(dtype, d, hq, new, kv, bloc
     assert none.any()
     assert torch.isnan(o[none]).all() and torch.all(lse[none] == -float("inf"))
     assert torch.all((o - want).abs()[~none] <= tol[~none]) and torch.all((lse - l64).abs()[~none] <= ltol[~none])
+
+
+def test_scratch_of_the_callers():
+    """A workspace in host memory is refused by every call that takes one; one on the device serves all of them."""
+    pr = paged.Problem(22, "bf16", 64, 16, 4, 2, [1, 40], [500, 90])
+    kv_len, table = pr.args()
+    c, q, qs = pr.cache(signatures=True), pr.q.cuda(), pr.q_start.cuda()
+    c.sig.zero_()
+    sel = c.select(q, kv_len, table, 6, q_start=qs, q_block=16)
+    calls = (lambda ws: c.attention(q, kv_len, table, q_start=qs, ws=ws)[0], lambda ws: c.select(q, kv_len, table, 6, q_start=qs, q_block=16, ws=ws),
+             lambda ws: c.block_attention(q, kv_len, table, sel, q_start=qs, q_block=16, ws=ws)[0])
+    for call in calls:
+        with pytest.raises(AssertionError):
+            call(torch.empty(1 << 24, dtype=torch.uint8))
+        assert torch.equal(call(torch.empty(1 << 28, dtype=torch.uint8, device="cuda")), call(None))

@@ -59,3 +59,12 @@ def test_calls_too_large_for_one_launch_are_refused_before_any():
     assert choose(1 << 13, 1 << 10, 1024) == -1
     assert b"too many" in s3.lib().s3_last_error()
     assert choose(1 << 15, 8, 1 << 20) == -1 and choose(1, 1, 1 << 30) == -1
+
+
+def test_scratch_in_host_memory_is_refused():
+    """A kernel would follow its address."""
+    import torch
+    q, c = torch.zeros(1, 8, 128), s3.KVCache.__new__(s3.KVCache)
+    with pytest.raises(AssertionError):
+        c._out(q, None, True, 256, torch.zeros(4096, dtype=torch.uint8))
+    assert c._out(q, None, False, 0, None)[2] is None
