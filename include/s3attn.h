@@ -353,7 +353,7 @@ typedef struct {
  * counted), so row i of n stands at position kv_len[s] - n + i.  Position p lies in slot p % page_size of page
  * block_table[s * table_stride + p / page_size].
  *   q_start      [n_seq + 1] int32, never descending, q_start[n_seq] <= n_tokens; NULL: one new token per sequence, n_tokens == n_seq
- *   kv_len       [n_seq] int32;  block_table [n_seq][table_stride] int32, max_pages entries of a row used
+ *   kv_len       [n_seq] int32;  block_table [n_seq][table_stride] int32, max_pages entries of a row used (none: may be NULL)
  *   max_new, max_kv   bounds of a sequence's new tokens and of kv_len: they size workspaces and share out the work, and
  *                what goes beyond them may be left out
  * Host structs of device pointers; the arrays are read when the kernels run.  What they hold cannot be checked on

@@ -308,7 +308,7 @@ int s3_kv_check(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b) {
     if (b->n_seq > 1 << 20 || b->n_tokens > 1 << 24 || (int64_t)b->max_pages * c->page_size > 1 << 30)
         return s3_fail(S3_EINVAL, "%s: n_seq %d, n_tokens %d or max_pages %d too large", fn, b->n_seq, b->n_tokens, b->max_pages);
     if (!b->q_start && b->n_tokens != b->n_seq) return s3_fail(S3_EINVAL, "%s: without q_start there is one token per sequence", fn);
-    if (b->n_seq && (!b->kv_len || !b->block_table)) return s3_fail(S3_EINVAL, "%s: null kv_len or block_table", fn);
+    if (b->n_seq && (!b->kv_len || (!b->block_table && b->max_pages))) return s3_fail(S3_EINVAL, "%s: null kv_len or block_table", fn);
     return S3_OK;
 }
 

@@ -77,3 +77,18 @@ def test_scratch_of_the_callers():
         with pytest.raises(AssertionError):
             call(torch.empty(1 << 24, dtype=torch.uint8))
         assert torch.equal(call(torch.empty(1 << 28, dtype=torch.uint8, device="cuda")), call(None))
+
+
+@pytest.mark.parametrize("new", [[1, 2], [90, 1]])
+def test_sequences_without_pages(new):
+    """A table of no columns: nothing is stored, every row sees nothing, no block is listed."""
+    pr = paged.Problem(23, "bf16", 64, 16, 4, 2, new, [100, 3])
+    c, q, qs, kv_len = pr.cache(signatures=True), pr.q.cuda(), pr.q_start.cuda(), pr.kv_len.cuda()
+    before = [t.clone() for t in (c.k, c.v)]
+    table = torch.empty(2, 0, dtype=torch.int32, device="cuda")
+    c.append(q[:, :2], q[:, 2:], kv_len, table, q_start=qs)
+    assert torch.equal(c.k, before[0]) and torch.equal(c.v, before[1])
+    sel = c.select(q, kv_len, table, 5, q_start=qs, q_block=16)
+    assert torch.all(sel == -1)
+    for o, lse in (c.attention(q, kv_len, table, q_start=qs, want_lse=True), c.block_attention(q, kv_len, table, torch.zeros_like(sel), q_start=qs, q_block=16, want_lse=True)):
+        assert torch.all(o == 0) and torch.all(lse == -float("inf"))

@@ -68,3 +68,10 @@ def test_scratch_in_host_memory_is_refused():
     with pytest.raises(AssertionError):
         c._out(q, None, True, 256, torch.zeros(4096, dtype=torch.uint8))
     assert c._out(q, None, False, 0, None)[2] is None
+
+
+def test_a_table_without_columns_is_no_error():
+    """Sequences that have no page yet: the table is empty, and so is its address."""
+    L, b = s3.lib(), batch(table=0, max_pages=0, stride=0)
+    assert L.s3_paged_attention_workspace(cache(), b, 8) > 0 and L.s3_block_attention_workspace(cache(), b, 8, 1, 4) > 0
+    assert L.s3_paged_attention_workspace(cache(), batch(table=0, max_pages=1, stride=1), 8) == 0
