@@ -21,14 +21,16 @@ import paper_2601_17702_amd as s3  # noqa: E402
 
 
 def span_blocks(starts, span_len: int, page: int, last_block: int, top: int, device):
-    """Blocks that the spans lie in, the first and the newest two, each once, in ascending order, -1 filled: [top] int32."""
+    """The first block and the newest two, then the blocks that the spans lie in, best span first, as far as `top` goes (top >= 3): each
+    once, in ascending order, -1 filled: [top] int32."""
     per = (span_len + page - 2) // page + 1
-    first = torch.div(starts.clamp(min=0), page, rounding_mode="floor")
-    blk = (first[:, None] + torch.arange(per, device=device)[None]).masked_fill((starts < 0)[:, None], last_block)
-    mark = torch.zeros(last_block + 1, dtype=torch.bool, device=device)
-    mark[blk.clamp(max=last_block).flatten()] = True
-    mark[0] = mark[-1] = mark[max(last_block - 1, 0)] = True
-    order = torch.where(mark, torch.arange(last_block + 1, device=device), last_block + 1).sort().values[:top]
+    blk = torch.div(starts, page, rounding_mode="floor")[:, None] + torch.arange(per, device=device)[None]
+    out_of_span = (starts < 0)[:, None] | (blk * page >= starts[:, None] + span_len) | (blk > last_block)
+    blk = torch.cat([torch.tensor([0, last_block, max(last_block - 1, 0)], device=device), blk.masked_fill(out_of_span, 0).flatten()])
+    none = blk.numel()
+    at = torch.full((last_block + 1,), none, device=device).scatter_reduce(0, blk, torch.arange(none, device=device), "amin")     # first named where
+    at, order = at.sort()
+    order = torch.where(at < none, order, last_block + 1)[:top].sort().values
     out = torch.full((top,), -1, dtype=torch.int32, device=device)
     out[:order.numel()] = torch.where(order <= last_block, order, -1).to(torch.int32)
     return out
