@@ -92,3 +92,106 @@ def test_sequences_without_pages(new):
     assert torch.all(sel == -1)
     for o, lse in (c.attention(q, kv_len, table, q_start=qs, want_lse=True), c.block_attention(q, kv_len, table, torch.zeros_like(sel), q_start=qs, q_block=16, want_lse=True)):
         assert torch.all(o == 0) and torch.all(lse == -float("inf"))
+
+
+# ------------------------------------------------------------------------------------------------ what the kernels hold inside the arrays
+def guarded(*shape, dtype, value):
+    """(whole, inner): an array with 64 rows of `value` before and behind it, all of it `value`."""
+    whole = torch.full((shape[0] + 128, *shape[1:]), value, dtype=dtype, device="cuda")
+    return whole, whole[64:64 + shape[0]]
+
+
+@pytest.mark.parametrize("dtype,new,kv", [("bf16", [1, 3], [70, 40]), ("bf16", [90, 2], [300, 31]), ("fp32", [40, 1], [64, 9])])
+def test_rows_of_no_sequence_are_not_written(dtype, new, kv):
+    """q_start begins at 3 and ends 5 rows before n_tokens."""
+    import paper_2601_17702_amd as s3
+    pr = paged.Problem(24, dtype, 64, 16, 4, 2, new, kv, garbage=2.0)
+    c, table, kv_len = pr.cache(signatures=True), pr.table.cuda(), pr.kv_len.cuda()
+    kc, vc = c.k.clone(), c.v.clone()
+    T = pr.T + 8
+    mine = torch.zeros(T, dtype=torch.bool)
+    mine[3:3 + pr.T] = True
+    q = torch.full((T, 4, 64), 7.0, dtype=pr.dtype)
+    q[mine] = pr.q
+    rows = [torch.full((T, 2, 64), 7.0, dtype=pr.dtype) for _ in range(2)]
+    for x, r in zip(rows, (pr.rows_k, pr.rows_v)):
+        x[mine] = torch.cat([r[s][m - n:] for s, (n, m) in enumerate(zip(new, kv))])          # the rows that are there already
+    qs = (pr.q_start + 3).cuda()
+    whole, out = guarded(T, 4, 64, dtype=pr.dtype, value=9.0)
+    got = c.append(rows[0].cuda(), rows[1].cuda(), kv_len, table, q_start=qs, q=q.cuda(), q_out=out)
+    assert torch.equal(out[mine.cuda()].cpu(), pr.q) and torch.all(whole[:67] == 9) and torch.all(whole[67 + pr.T:] == 9) and got is out
+    assert torch.equal(c.k, kc) and torch.equal(c.v, vc)
+    want = paged.attend(pr)
+    whole, out = guarded(T, 4, 64, dtype=pr.dtype, value=9.0)
+    _, lse = c.attention(q.cuda(), kv_len, table, q_start=qs, out=out, want_lse=True)
+    paged.check(pr, out[mine.cuda()], lse[mine.cuda()], want)
+    assert torch.all(whole[:67] == 9) and torch.all(whole[67 + pr.T:] == 9)
+    tiles = s3.lib().s3_block_tiles(c._batch(T, kv_len, table, qs, None, None), 16)
+    sel = torch.arange(table.shape[1], dtype=torch.int32, device="cuda").repeat(tiles, 2, 1).contiguous()
+    whole, out = guarded(T, 4, 64, dtype=pr.dtype, value=9.0)
+    _, lse = c.block_attention(q.cuda(), kv_len, table, sel, q_start=qs, q_block=16, out=out, want_lse=True)
+    paged.check(pr, out[mine.cuda()], lse[mine.cuda()], want)
+    assert torch.all(whole[:67] == 9) and torch.all(whole[67 + pr.T:] == 9)
+    sig = torch.from_numpy(paged.grid8(torch.randn(pr.n_pages, 2, 64, generator=pr.g).numpy())).to(torch.bfloat16)
+    c.sig.copy_(sig)
+    got = c.select(q.cuda(), kv_len, table, 5, q_start=qs, q_block=16).cpu().numpy()
+    ref = paged.select(pr, sig, 5, 16, 1, 1)
+    n = sum(-(-x // 16) for x in new)
+    assert (got[:n] == ref[:n]).all() and (got[n:] == -1).all()
+
+
+@pytest.mark.parametrize("starts", [[0, 5, 60, 60], [0, 30, 10, 40], [0, 40, 90, 100], [2, -3, 8, 40]])
+def test_starts_that_are_no_starts_write_nothing_else(starts):
+    """Starts past n_tokens, that descend or are negative: which rows are written is open, but only rows of the call, lists that it has and pages of its
+    tables are."""
+    import paper_2601_17702_amd as s3
+    T, P = 40, 16
+    pr = paged.Problem(25, "bf16", 64, P, 4, 2, [20, 10, 10], [100, 60, 40])
+    qs = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    kv_len, table = pr.args()
+    q = pr.q.cuda()
+    c = pr.cache(signatures=True)
+    c.sig.zero_()
+    unused = [p for p in range(pr.n_pages) if p not in set(pr.table.flatten().tolist())]
+    before = [t[unused].clone() for t in (c.k, c.v, c.sig)]
+    whole, out = guarded(T, 4, 64, dtype=pr.dtype, value=9.0)
+    c.append(q[:, :2], q[:, 2:], kv_len, table, q_start=qs, q=q, q_out=out)
+    assert torch.all(whole[:64] == 9) and torch.all(whole[64 + T:] == 9)
+    assert all(torch.equal(t[unused], b) for t, b in zip((c.k, c.v, c.sig), before))
+    for max_new in (40, 4):
+        whole, out = guarded(T, 4, 64, dtype=pr.dtype, value=9.0)
+        c.attention(q, kv_len, table, q_start=qs, max_new=max_new, out=out)
+        assert torch.all(whole[:64] == 9) and torch.all(whole[64 + T:] == 9)
+        for qb in (1, 8, 40):
+            sel = c.select(q, kv_len, table, 6, q_start=qs, q_block=qb, lead=1, tail=0, max_new=max_new)
+            assert torch.all((sel >= -1) & (sel < table.shape[1]))
+            whole, lists = guarded(*sel.shape, dtype=torch.int32, value=-9)
+            b = c._batch(T, kv_len, table, qs, max_new, None)
+            ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+            assert s3.lib().s3_block_select(c._c, b, q.data_ptr(), 4, q.stride(0), q.stride(1), qb, 6, 1, 0, lists.data_ptr(), ws.data_ptr(), 1 << 24, s3._stream()) == 0
+            assert torch.equal(lists, sel) and torch.all(whole[:64] == -9) and torch.all(whole[64 + len(sel):] == -9)
+            whole, out = guarded(T, 4, 64, dtype=pr.dtype, value=9.0)
+            c.block_attention(q, kv_len, table, sel, q_start=qs, q_block=qb, max_new=max_new, out=out)
+            assert torch.all(whole[:64] == 9) and torch.all(whole[64 + T:] == 9)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_explicit_positions_outside_the_table(inter):
+    """They are taken as the table's first or last row: in the four-token path, in the others and for keys."""
+    import paper_2601_17702_amd as s3
+    T, n_pos = 600, 50
+    pr = paged.Problem(26, "bf16", 128, 64, 32, 2, [T], [T])
+    c = pr.cache(signatures=True)
+    pos = torch.randint(-60, 120, (T,), generator=pr.g, dtype=torch.int32)
+    pos[:4] = torch.tensor([-(1 << 31), (1 << 31) - 1, -1, n_pos])
+    rope = s3.rope_table(n_pos, 128)
+    args = dict(q_start=pr.q_start.cuda(), rope=rope, interleaved=inter, q=pr.q.cuda())
+    k = torch.cat(pr.rows_k).cuda()
+    caches = []
+    for p in (pos, pos.clamp(0, n_pos - 1)):
+        out = c.append(k, k, pr.kv_len.cuda(), pr.table.cuda(), positions=p.cuda(), **args)
+        caches.append((out.clone(), c.k.clone(), c.sig.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*caches))
+    short = s3.rope_table(T, 128)                                      # positions inside: another result
+    out = c.append(k, k, pr.kv_len.cuda(), pr.table.cuda(), **{**args, "rope": short})
+    assert not torch.equal(out, caches[0][0])
