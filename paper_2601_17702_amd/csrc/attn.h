@@ -35,7 +35,7 @@ struct AttnArgs {
     const int32_t* sel;       // block lists, or null: all blocks
     int64_t q_ts, q_hs;       // bytes
     int n_kv, G, n_q, window;
-    int qb, top, per_q, lists;// lists: tokens a tile, entries, row tiles a tile of queries, how many lists there are
+    int qb, top, per_q, lists;// lists: tokens a tile, entries, row tiles a tile of queries (tiled kernel), how many lists there are
     float sl;                 // scale * log2(e)
     int few;                  // sequences of at most this many rows are the streaming kernel's
 };

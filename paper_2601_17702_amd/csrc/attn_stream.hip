@@ -29,7 +29,7 @@ __device__ __forceinline__ int64_t wave_incl_scan64(int64_t x) {
 // fp32 of a scratch slot: R rows' sums, their maxima and the weights' sums; whole 16-byte pieces, for R may be odd.
 __host__ __device__ __forceinline__ int64_t slot_floats(int R, int D) { return ((int64_t)R * (D + 2) + 3) & ~(int64_t)3; }
 
-// A sequence's part of the line: tiles of rows, each with n_kv heads of `pieces` pieces that begin at token lo.
+// A sequence's part of the line: row tiles (one, or one a tile of listed blocks), each with n_kv heads of `pieces` pieces that begin at token lo.
 struct Part {
     int first, n, len, lo, tiles, pieces;
 };
@@ -39,10 +39,10 @@ __device__ __forceinline__ Part part_of(const AttnArgs& p, int s) {
     kv_seq(p.b, s, r.first, r.n, r.len);
     r.lo = 0;
     if (LIST) {
-        r.tiles = (r.n + p.qb - 1) / p.qb * p.per_q;
+        r.tiles = (r.n + p.qb - 1) / p.qb;
         r.pieces = ((p.top << p.b.log_page) + kPiece<RT> - 1) / kPiece<RT>;
     } else {
-        r.tiles = r.n * p.G <= p.few ? (r.n * p.G + 32 * RT - 1) / (32 * RT) : 0;
+        r.tiles = r.n > 0 && r.n * p.G <= p.few ? 1 : 0;
         if (p.window) r.lo = max(0, r.len - r.n - p.window + 1) & ~31;
         const int hi = min(r.len, kv_blocks(p.b, r.len) << p.b.log_page);
         r.pieces = (max(hi - r.lo, 1) + kPiece<RT> - 1) / kPiece<RT>;         // one at least: rows that see nothing are written, too
@@ -50,17 +50,11 @@ __device__ __forceinline__ Part part_of(const AttnArgs& p, int s) {
     return r;
 }
 
-// Rows of a tile: the first, and the end.
+// Rows of a tile: the first, and the end (32 RT of them at most, as the host saw to it).
 template <bool LIST, int RT>
 __device__ __forceinline__ void rows_of(const AttnArgs& p, const Part& part, int tile, int& r0, int& r_end) {
-    if (LIST) {
-        const int qt = tile / p.per_q;
-        r0 = qt * p.qb * p.G + (tile - qt * p.per_q) * (32 * RT);
-        r_end = min(min(part.n, (qt + 1) * p.qb) * p.G, r0 + 32 * RT);
-    } else {
-        r0 = tile * (32 * RT);
-        r_end = min(part.n * p.G, r0 + 32 * RT);
-    }
+    r0 = __builtin_amdgcn_readfirstlane(LIST ? tile * p.qb * p.G : 0);
+    r_end = __builtin_amdgcn_readfirstlane(min((LIST ? min(part.n, (tile + 1) * p.qb) : part.n) * p.G, r0 + 32 * RT));
 }
 
 // The line's length and equal runs of it.
@@ -139,10 +133,12 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
             tile0 += part.tiles;
             continue;
         }
-        const int c0 = (int)(rem % part.pieces);
+        // all lanes' values: in scalar registers, for the vector ones are all in use
+        const int c0 = __builtin_amdgcn_readfirstlane((int)(rem % part.pieces));
         const int64_t u = rem / part.pieces;
-        const int tile = (int)(u / p.n_kv), head = (int)(u % p.n_kv);
-        const int c1 = (int)min((int64_t)part.pieces, c0 + (end - at));
+        const int tile = LIST ? __builtin_amdgcn_readfirstlane((int)(u / p.n_kv)) : 0;
+        const int head = __builtin_amdgcn_readfirstlane(LIST ? (int)(u % p.n_kv) : (int)u);
+        const int c1 = __builtin_amdgcn_readfirstlane((int)min((int64_t)part.pieces, c0 + (end - at)));
 
         int r0, r_end;
         rows_of<LIST, RT>(p, part, tile, r0, r_end);
@@ -155,8 +151,8 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         const int last = part.len - part.n + (r_end - 1) / p.G;                   // the last row's; its tokens end at hi
         const int hi = min(last + 1, kv_blocks(p.b, part.len) << logp);
         const AttnSight sight(rows.pos, hi, p.window);
-        const int32_t* list = LIST ? p.sel + ((int64_t)((tile0 + tile) / p.per_q) * p.n_kv + head) * p.top : nullptr;
-        const int n_list = LIST && (tile0 + tile) / p.per_q < p.lists ? p.top << (logp - 4) : 0;
+        const int32_t* list = LIST ? p.sel + ((int64_t)(tile0 + tile) * p.n_kv + head) * p.top : nullptr;
+        const int n_list = LIST && tile0 + tile < p.lists ? p.top << (logp - 4) : 0;
         for (int cb = c0; cb < c1; cb += kBatchRuns / RUNS) {
             int n = min(c1 - cb, kBatchRuns / RUNS) * RUNS;
             __syncthreads();                                                       // the last batch, the last tile's sums are read
@@ -215,9 +211,9 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
             load_v(ra, rb, 0);
             for (int i = 0; i < n_sub; ++i) {
                 const int2 a = ra, b = rb;
-                kv_f32x16 sc[1];
+                kv_f32x16 sc;
 #pragma unroll
-                for (int x = 0; x < 16; ++x) sc[0][x] = 0.0f;
+                for (int x = 0; x < 16; ++x) sc[x] = 0.0f;
 #pragma unroll
                 for (int part = 0; part < VC; ++part) {
                     if (part) {
@@ -225,7 +221,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                         __builtin_amdgcn_sched_barrier(0);
                     }
 #pragma unroll
-                    for (int q = 0; q < QC; ++q) sc[0] = kv_mma(kf[q], rows.q[part * QC + q], sc[0]);
+                    for (int q = 0; q < QC; ++q) sc = kv_mma(kf[q], rows.q[part * QC + q], sc);
                     if (VC > 1) __builtin_amdgcn_sched_barrier(0);
                 }
                 const bool more = i + 1 < n_sub;
@@ -242,18 +238,18 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                         const int t = 2 * E * (x / E) + E * half + x % E;
                         const bool sees = sight.sees((2 * E * (x / E) < 16 ? a.x : b.x) + (t & 15));
                         seen |= sees;
-                        sc[0][x] = sees ? sc[0][x] : -INFINITY;
+                        sc[x] = sees ? sc[x] : -INFINITY;
                     }
                 } else {
                     seen = true;
                 }
-                float x = sc[0][0];
+                float x = sc[0];
 #pragma unroll
-                for (int e = 1; e < 16; ++e) x = fmaxf(x, sc[0][e]);
+                for (int e = 1; e < 16; ++e) x = fmaxf(x, sc[e]);
                 const float sub = st.advance(x, p.sl);
                 vec w[NW];
 #pragma unroll
-                for (int y = 0; y < NW; ++y) w[y] = st.weights(sc[0], y, p.sl, sub);
+                for (int y = 0; y < NW; ++y) w[y] = st.weights(sc, y, p.sl, sub);
 #pragma unroll
                 for (int part = 0; part < VC; ++part) {
                     if (part) {

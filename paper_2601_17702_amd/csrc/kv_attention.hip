@@ -48,13 +48,11 @@ struct Plan {
         // no sequence is a short one if even the others at their longest leave more rows for it
         const bool all_long = b->n_tokens > (int64_t)(b->n_seq - 1) * b->max_new + limit / G;
         few = !many || (!q_block && !all_long);
-        // row tiles of 32, 64 or 128 rows: one whenever they go into one
-        R = (int)min(most, (int64_t)limit);
-        const int tile = R <= 32 ? 32 : R <= 64 ? 64 : 128;
+        R = (int)min(most, (int64_t)limit);                    // a sequence's, or a tile of listed blocks', are one row tile
         few_ws = few ? s3_attn_stream_workspace(c->d_head, R) : 0;
         const int rows = s3_attn_tile_rows(c);
-        per_q = !q_block ? 1 : (int)((most + (many ? rows : tile) - 1) / (many ? rows : tile));
-        few_tiles = q_block ? s3_block_tiles(b, q_block) * per_q : min(((int64_t)b->n_tokens * G + (int64_t)min(b->n_seq, b->n_tokens) * (tile - 1)) / tile, (int64_t)b->n_seq);
+        per_q = (int)((most + rows - 1) / rows);
+        few_tiles = q_block ? s3_block_tiles(b, q_block) : min(b->n_seq, b->n_tokens);
         // row tiles that there can be: beside the streaming kernel only sequences of more than `limit` rows have any, and each ends in one
         // that is not full; none has more than max_new tokens
         const int64_t all = (int64_t)b->n_tokens * G, longs = min((int64_t)min(b->n_seq, b->n_tokens), few ? all / (limit + 1) : all);
