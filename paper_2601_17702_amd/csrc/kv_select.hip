@@ -643,9 +643,13 @@ struct SelectPlan {
         groups = (tiles + (int64_t)b->n_seq * (t - 1)) / t;
         whole = q_block <= most && (int64_t)q_block * G % 32 == 0;
         waves = sets == 1 && groups * c->n_kv_heads < 256 ? 16 : 8;
-        // one tile a workgroup: 512 lists of 62 / 500 candidates 14 / 25.3 us in one kernel, 12.1 / 27.4 through scratch; 8 of 500, 18 / 12.5
+        // One kernel or scratch between two, us a call.  One tile of few rows a workgroup: the first wants a workgroup for every compute unit, and lists that are
+        // worth its longer beginning (lists x candidates, one kernel / scratch: 64 x 2000 33 / 22, 64 x 8000 98 / 48, 128 x 500 18 / 13, 128 x 3000 44 / 37,
+        // 256 x 300 14.7 / 13.8, 256 x 500 15.7 / 15.8, 256 x 2000 33 / 39, 512 x 200 17 / 15, 512 x 400 19 / 21, 512 x 2000 47 / 65, 1024 x 300 30 / 30,
+        // 4096 x 100 92 / 48, 4096 x 500 123 / 138).  More rows, which scratch reads from every workgroup of a list: 64 rows, 8 x 200 13 / 15,
+        // 8 x 500 16 / 16, 8 x 2000 36 / 22, 64 x 2000 36 / 32, 128 x 2000 37 / 47; 256 rows, 8 x 500 25 / 32, 8 x 2000 63 / 38, 64 x 2000 63 / 75.
         const int64_t lists = groups * c->n_kv_heads;
-        fused = nb <= 30720 && (sets == 1 && tiles_wg == 1 ? lists * nb >= 200000 : lists >= 64 || nb <= 256);
+        fused = nb <= 30720 && (sets == 1 && tiles_wg == 1 ? lists >= 256 && nb >= 400 : lists >= 64 || nb <= 256);
     }
     size_t workspace(int n_kv) const { return fused ? 0 : s3_align((size_t)tiles * n_kv * nb * 4); }
 };
@@ -673,7 +677,7 @@ int launch_select(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
     const dim3 grid((unsigned)(plan.tiles * p.n_kv), (unsigned)((p.nb + kScoreBlocks - 1) / kScoreBlocks));
     hipLaunchKernelGGL((sel_score_kernel<T, D>), grid, dim3(kThreads), 0, st, p);
     S3_HIP(hipGetLastError());
-    // 8 lists of 2048 / 15625 candidates, us a call: 21 / 86 with the first, 32 / 41 with the second
+    // us a call with the first / the second: 8 lists of 3000 candidates 22 / 24, 4096 25 / 25, 8000 45 / 25; 64 of 3000 29 / 32, 4096 35 / 35, 8000 66 / 48
     if (p.nb <= 4096) hipLaunchKernelGGL(sel_pick_kernel, dim3(grid.x), dim3(kThreads), 0, st, p);
     else hipLaunchKernelGGL(sel_pick_long_kernel, dim3(grid.x), dim3(kPickWaves * 64), 0, st, p);
     S3_HIP(hipGetLastError());

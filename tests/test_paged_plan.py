@@ -75,3 +75,15 @@ def test_a_table_without_columns_is_no_error():
     L, b = s3.lib(), batch(table=0, max_pages=0, stride=0)
     assert L.s3_paged_attention_workspace(cache(), b, 8) > 0 and L.s3_block_attention_workspace(cache(), b, 8, 1, 4) > 0
     assert L.s3_paged_attention_workspace(cache(), batch(table=0, max_pages=1, stride=1), 8) == 0
+
+
+def test_which_choices_go_through_scratch():
+    """Scores of a decoding batch's lists are left in scratch unless there is a list for every compute unit, and 400 candidates in it."""
+    def scratch_of(n_seq, nb, max_new=1, n_tokens=None, q_block=1, heads=8):
+        b = batch(n_seq=n_seq, n_tokens=n_tokens or n_seq, max_new=max_new, max_pages=nb, stride=nb, max_kv=nb * 64)
+        return s3.lib().s3_block_select_workspace(cache(heads=heads), b, 32, q_block, 32)
+    for n_seq, nb in ((8, 2000), (8, 8000), (16, 3000), (32, 300), (512, 100), (1, 100)):
+        assert scratch_of(n_seq, nb) >= n_seq * 8 * nb * 4, (n_seq, nb)
+    for n_seq, nb in ((32, 500), (64, 512), (512, 500), (64, 8000)):
+        assert scratch_of(n_seq, nb) == 0, (n_seq, nb)
+    assert scratch_of(1, 2000, 16, 16, 16) > 0 and scratch_of(1, 200, 16, 16, 16) == 0 and scratch_of(1, 2000, 256, 256, 16) == 0
