@@ -61,12 +61,10 @@ struct Plan {
         const int64_t all = (int64_t)b->n_tokens * G, longs = min((int64_t)min(b->n_seq, b->n_tokens), few ? all / (limit + 1) : all);
         many_tiles = !many ? 0 : q_block ? s3_block_tiles(b, q_block) * per_q : min((all + longs * (rows - 1)) / rows, longs * ((most + rows - 1) / rows));
         const int64_t units = many_tiles * c->n_kv_heads, tokens = q_block ? (int64_t)top_b * c->page_size : b->max_kv;
-        // Every tile that there can be weighs the same, for the host knows no sequence's own length.  Weighed by the longest chunk's tiles alone, 2048 tokens
-        // at 2048 beside eight times 30 at 131072 took 2546 us instead of 1293 (the short ones' tiles see most), 256 at 131072 beside 42 single
-        // tokens 791 instead of 1027.
-        n_split = many ? s3_attn_tile_split(c, units, tokens) : 1;
+        const bool ragged = !q_block && b->n_seq > 1;
+        n_split = many ? s3_attn_tile_split(c, units, tokens, ragged) : 1;
         many_ws = s3_attn_tile_workspace(c, units, n_split);              // for any window
-        if (many && window) n_split = min(n_split, s3_attn_tile_split(c, units, min(tokens, (int64_t)window + rows / G)));
+        if (many && window) n_split = min(n_split, s3_attn_tile_split(c, units, min(tokens, (int64_t)window + rows / G), ragged));
     }
 };
 
