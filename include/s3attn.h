@@ -355,7 +355,8 @@ typedef struct {
  *   q_start      [n_seq + 1] int32, never descending, q_start[n_seq] <= n_tokens; NULL: one new token per sequence, n_tokens == n_seq
  *   kv_len       [n_seq] int32;  block_table [n_seq][table_stride] int32, max_pages entries of a row used (none: may be NULL)
  *   max_new, max_kv   bounds of a sequence's new tokens and of kv_len: they size workspaces and share out the work, and
- *                what goes beyond them may be left out
+ *                what goes beyond them may be left out.  Loose ones cost: attention of single tokens with q_start and max_new = n_tokens
+ *                plans for chunks beside them, one launch more and up to some hundred MB of workspace
  * Host structs of device pointers; the arrays are read when the kernels run.  What they hold cannot be checked on
  * the host: tokens past n_tokens are left out, a position whose block is beyond max_pages or whose page number is outside
  * [0, n_pages) is not stored and is masked for every reader, and rows of no sequence are not written.
@@ -401,8 +402,10 @@ int s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const void*
  *   j > p - window where window > 0; G = n_q_heads / n_kv_heads.
  *   lse[t, h] = log sum_j exp(scale q . k) (natural log), or NULL.
  * A row that sees nothing (kv_len smaller than the number of new tokens, unmapped pages) is 0 with lse -inf; one that sees tokens, but
- * scores of -inf only, is NaN with lse -inf.  Values in masked places never reach a row, infinities and NaN included.
- * Softmax statistics and sums in fp32; with bf16 the weights are rounded to bf16 for the second product.
+ * scores of -inf only, is NaN with lse -inf.  Values in masked places never reach a row, infinities and NaN included.  An infinite value that
+ * a row sees makes its channel infinite, or NaN where fp32 does not hold the value's weight (which of the two depends on how the call is cut).
+ * Softmax statistics and sums in fp32; with bf16 the weights are rounded to bf16 for the second product, their sum is not: outputs are
+ * within 2^-8 of the weighted sum of magnitudes, and once more 2^-8 of themselves by their own rounding.
  *   q    [n_tokens][n_q_heads][d_head], strides as in s3_kv_append;  out [n_tokens][n_q_heads][d_head] contiguous, dtype
  *   ws   s3_paged_attention_workspace(...) bytes, 256-byte aligned, contents meaningless between calls
  * Limits: 1 <= G <= 32; scale > 0; window >= 0.  n_kv_heads times n_seq below 2^22, and times the chunks' tiles of 128 rows (n_tokens * G / 128,

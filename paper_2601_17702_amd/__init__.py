@@ -486,7 +486,8 @@ class KVCache:
 
     Arguments that the calls share: kv_len [n_seq] int32, the sequences' lengths with the new tokens counted; block_table
     [n_seq, max_pages] int32, page numbers; q_start [n_seq + 1] int32, rows of the new tokens (None: one per sequence); max_new and
-    max_kv, bounds of the new tokens and of kv_len that the host knows (they share out the work).  Arrays of rows are [n_tokens, heads, d_head],
+    max_kv, bounds of the new tokens and of kv_len that the host knows (they share out the work; give max_new with q_start, without it
+    a batch of single tokens is planned as if chunks were among them, with their launch and workspace).  Arrays of rows are [n_tokens, heads, d_head],
     the last axis contiguous, the others of any stride that is a multiple of 16 bytes."""
 
     def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, dtype=None, signatures: bool = False,

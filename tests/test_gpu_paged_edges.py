@@ -195,3 +195,25 @@ def test_explicit_positions_outside_the_table(inter):
     short = s3.rope_table(T, 128)                                      # positions inside: another result
     out = c.append(k, k, pr.kv_len.cuda(), pr.table.cuda(), **{**args, "rope": short})
     assert not torch.equal(out, caches[0][0])
+
+
+@pytest.mark.parametrize("dtype,d,new,kv", [("bf16", 64, [1], [70]), ("bf16", 128, [1], [3000]), ("bf16", 128, [150], [200]), ("fp32", 64, [90], [90]), ("fp32", 256, [3], [40])])
+def test_an_infinite_value_of_next_to_no_weight(dtype, d, new, kv):
+    """A token with a score hundreds below the others', an infinite value in one of its channels: that channel is infinite or NaN for the
+    rows that see it, wherever in the call the token lies, the other channels are as without it."""
+    for at in (0, kv[0] - new[0] // 2 - 1):
+        pr = paged.Problem(27 + d, dtype, d, 32, 4, 2, new, kv)
+        pr.q[..., 0] = 4.0
+        pr.rows_k[0][..., 0] = 0.0
+        pr.rows_k[0][at, :, 0] = -400.0                                # scaled by 1 below: 1600 under the others
+        pr.rows_v[0][at, :, 5] = float("inf")
+        kv_len, table = pr.args()
+        o, _ = pr.cache().attention(pr.q.cuda(), kv_len, table, q_start=pr.q_start.cuda(), scale=1.0)
+        o = o.cpu().to(torch.float64)
+        sees = torch.arange(kv[0] - new[0], kv[0]) >= at
+        alone = (torch.arange(kv[0] - new[0], kv[0]) == 0) & (at == 0)  # a prompt's first row sees nothing else
+        assert not torch.isfinite(o[sees][:, :, 5]).any() and torch.isfinite(o[~sees]).all()
+        pr.rows_v[0][at, :, 5] = 0.0
+        want, _, tol, _ = paged.attend(pr, scale=1.0)
+        rest = torch.arange(d) != 5
+        assert torch.all((o - want).abs()[:, :, rest] <= tol[:, :, rest]) and (not alone.any() or torch.isinf(o[alone][:, :, 5]).all())
