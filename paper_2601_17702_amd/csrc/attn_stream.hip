@@ -115,11 +115,11 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
                 const int l = __builtin_ctzll(__ballot(run + incl > at));
                 s = base + l;
                 rem = at - (run + __shfl(incl, l) - __shfl(c, l));
-                if (LIST) tile0 += __builtin_amdgcn_readlane(t_incl, l) - __builtin_amdgcn_readlane(tiles, l);
+                if (LIST) tile0 = kv_add_lists(tile0, __builtin_amdgcn_readlane(t_incl, l) - __builtin_amdgcn_readlane(tiles, l));
                 break;
             }
             run += sum;
-            if (LIST) tile0 += __builtin_amdgcn_readlane(t_incl, 63);
+            if (LIST) tile0 = kv_add_lists(tile0, __builtin_amdgcn_readlane(t_incl, 63));
         }
         s = __builtin_amdgcn_readfirstlane(s);
     }
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kThreads, D * sizeof(T) > 256 ? 1 : 2) void attn_st
         if (rem >= size) {
             ++s;
             rem = 0;
-            tile0 += part.tiles;
+            tile0 = kv_add_lists(tile0, part.tiles);
             continue;
         }
         // all lanes' values: in scalar registers, for the vector ones are all in use

@@ -41,6 +41,9 @@ __device__ __forceinline__ void kv_seq(const KvBatch& b, int s, int& first, int&
     }
     len = max(0, min(b.kv_len[s], 1 << 30));
 }
+// Counts of lists summed over sequences: where starts descend the sum may be any number, and an index made of it must not wrap to below the
+// array.  64 sequences have 2^30 lists at most.
+__device__ __forceinline__ int kv_add_lists(int all, int more) { return min(all + more, 1 << 29); }
 // Blocks that hold len tokens, as far as the table goes.
 __device__ __forceinline__ int kv_blocks(const KvBatch& b, int len) {
     return min((len + (1 << b.log_page) - 1) >> b.log_page, b.max_pages);

@@ -407,7 +407,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 || WAVES == 4 ? 2 : 4) void se
             len = __builtin_amdgcn_readlane(l, x);
             tile0 = tiles_all + __builtin_amdgcn_readlane(ci, x) - __builtin_amdgcn_readlane(c, x) + j * tiles_wg;
         }
-        tiles_all += __builtin_amdgcn_readlane(ci, 63);
+        tiles_all = kv_add_lists(tiles_all, __builtin_amdgcn_readlane(ci, 63));
         groups += g_sum;
     }
     if (group == 0)                                              // lists past the last tile

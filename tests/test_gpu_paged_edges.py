@@ -217,3 +217,21 @@ def test_an_infinite_value_of_next_to_no_weight(dtype, d, new, kv):
         want, _, tol, _ = paged.attend(pr, scale=1.0)
         rest = torch.arange(d) != 5
         assert torch.all((o - want).abs()[:, :, rest] <= tol[:, :, rest]) and (not alone.any() or torch.isinf(o[alone][:, :, 5]).all())
+
+
+def test_starts_whose_counts_pass_31_bits():
+    """2^15 sequences that all claim the same 2^16 tokens: the number of their lists wraps, where the array is written does not."""
+    import paper_2601_17702_amd as s3
+    T = n_seq = 1 << 16
+    c = s3.KVCache(1, 16, 1, 64, signatures=True)
+    c.sig.zero_()
+    qs = (torch.arange(n_seq + 1, device="cuda") % 2 * T).to(torch.int32)
+    kv_len = torch.full((n_seq,), 16, dtype=torch.int32, device="cuda")
+    table = torch.zeros(n_seq, 1, dtype=torch.int32, device="cuda")
+    q = torch.ones(T, 1, 64, dtype=torch.bfloat16, device="cuda")
+    b = c._batch(T, kv_len, table, qs, T, 16)
+    tiles = s3.lib().s3_block_tiles(b, 1)
+    whole, sel = guarded(tiles, 1, 4, dtype=torch.int32, value=-9)
+    assert s3.lib().s3_block_select_workspace(c._c, b, 1, 1, 4) == 0
+    assert s3.lib().s3_block_select(c._c, b, q.data_ptr(), 1, 64, 64, 1, 4, 1, 1, sel.data_ptr(), None, 0, s3._stream()) == 0
+    assert torch.all(whole[:64] == -9) and torch.all(whole[64 + tiles:] == -9) and torch.all((sel == -1) | (sel == 0))
