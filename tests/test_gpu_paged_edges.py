@@ -235,3 +235,13 @@ def test_starts_whose_counts_pass_31_bits():
     assert s3.lib().s3_block_select_workspace(c._c, b, 1, 1, 4) == 0
     assert s3.lib().s3_block_select(c._c, b, q.data_ptr(), 1, 64, 64, 1, 4, 1, 1, sel.data_ptr(), None, 0, s3._stream()) == 0
     assert torch.all(whole[:64] == -9) and torch.all(whole[64 + tiles:] == -9) and torch.all((sel == -1) | (sel == 0))
+
+
+@pytest.mark.parametrize("rot,theta", [(128, 10000.0), (64, 500000.0)])
+def test_rotation_table_of_far_positions(rot, theta):
+    """Angles up to 131071 radians: formed in 64 bits they are good to 1e-10, cos and sin are rounded once."""
+    import paper_2601_17702_amd as s3
+    n = 131072
+    table = s3.rope_table(n, rot, theta).cpu().to(torch.float64)
+    ang = torch.arange(n, dtype=torch.float64)[:, None] * theta ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    assert torch.all((table - torch.cat([ang.cos(), ang.sin()], 1)).abs() <= 2.0 ** -25 + 1e-9)
