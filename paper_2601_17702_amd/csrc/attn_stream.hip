@@ -1,7 +1,7 @@
 // Attention of few rows: sequences (or tiles of listed blocks) whose new tokens times query heads per key/value head are 128 at most.
 //
 // The work is one pass over the keys and values, so memory bounds it: 64 decoding steps of 300 to 32768 tokens (1.86 GB)
-// take 350 us, 5.3 TB/s (a copy moves 4.8).  All of it, over all sequences and heads, is one line of pieces of 128 tokens, and every
+// take 348 us with the join, 5.3 TB/s (a copy moves 4.8).  All of it, over all sequences and heads, is one line of pieces of 128 tokens, and every
 // workgroup takes an equal run of that line whatever the lengths are: a long sequence is shared by many workgroups, short ones lie
 // whole in one.  A workgroup's four wavefronts take 32 tokens of a piece each, keys and values straight from memory into the
 // matrix instructions' operands, the next 32 tokens' keys on their way while the weights are made and the next values
