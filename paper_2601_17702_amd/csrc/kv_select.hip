@@ -1,10 +1,10 @@
 // The blocks that each tile of queries will read (s3_block_select): scores of all candidates by matrix instructions, then the
-// top_b largest of each list by a radix search on the scores' ordered keys.
+// top_b largest of each list by a search for their threshold among the scores' ordered keys.
 //
 // Two forms.  sel_fused_kernel keeps a tile's keys in LDS: a workgroup takes some tiles of one sequence and head, all their rows in
 // registers, its wavefronts walk over different signatures, and a wavefront each then picks for a tile.  Where that would leave the
-// chip idle (few tiles, long contexts) or does not fit LDS, sel_score_kernel spreads the scores of a tile over many workgroups and leaves
-// the keys in scratch for sel_pick_kernel.
+// chip idle (few tiles), is not worth its longer beginning (few candidates) or does not fit LDS, sel_score_kernel spreads the scores of a tile over many
+// workgroups and leaves the keys in scratch for sel_pick_kernel or, from 4097 candidates on, sel_pick_long_kernel.
 //
 // Measured, 32 query heads over 8, d_head 128: 32 of up to 512 blocks for 64 decoding steps 19 us (37 MB of signatures would be 8; lengths,
 // table, signatures, scores and choice wait for each other); 64 of 2048 blocks for each 16 of 2048 queries 56 us, of which the scores are 44:
