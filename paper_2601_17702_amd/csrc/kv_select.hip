@@ -625,7 +625,7 @@ int select_blocks(const s3_kv_cache* c, const s3_kv_batch* b) {
 // How a call is shared out.
 struct SelectPlan {
     bool fused, whole;
-    int tiles_wg, sets, waves, nb;
+    int tiles_wg, sets, nb;
     int64_t tiles, groups;
     SelectPlan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block) {
         nb = select_blocks(c, b);
@@ -642,7 +642,6 @@ struct SelectPlan {
         sets = t * fours <= 8 ? 1 : t * fours <= 16 || max_sets == 2 ? 2 : 4;
         groups = (tiles + (int64_t)b->n_seq * (t - 1)) / t;
         whole = q_block <= most && (int64_t)q_block * G % 32 == 0;
-        waves = sets == 1 && groups * c->n_kv_heads < 256 ? 16 : 8;
         // One kernel or scratch between two, us a call.  One tile of few rows a workgroup: the first wants a workgroup for every compute unit, and lists that are
         // worth its longer beginning (lists x candidates, one kernel / scratch: 64 x 2000 33 / 22, 64 x 8000 98 / 48, 128 x 500 18 / 13, 128 x 3000 44 / 37,
         // 256 x 300 14.7 / 13.8, 256 x 500 15.7 / 15.8, 256 x 2000 33 / 39, 512 x 200 17 / 15, 512 x 400 19 / 21, 512 x 2000 47 / 65, 1024 x 300 30 / 30,
@@ -668,7 +667,6 @@ template <typename T, int D>
 int launch_select(const SelectArgs& p, const SelectPlan& plan, hipStream_t st) {
     if (plan.fused) {
         if constexpr (D < 256) {
-            if (plan.waves == 16) return launch_fused<T, D, 1, 16, false>(p, plan, st);
             if (plan.sets == 4) return plan.whole ? launch_fused<T, D, 4, 4, true>(p, plan, st) : launch_fused<T, D, 4, 4, false>(p, plan, st);
         }
         if (plan.sets == 1) return launch_fused<T, D, 1, 8, false>(p, plan, st);

@@ -245,3 +245,29 @@ def test_rotation_table_of_far_positions(rot, theta):
     table = s3.rope_table(n, rot, theta).cpu().to(torch.float64)
     ang = torch.arange(n, dtype=torch.float64)[:, None] * theta ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
     assert torch.all((table - torch.cat([ang.cos(), ang.sin()], 1)).abs() <= 2.0 ** -25 + 1e-9)
+
+
+@pytest.mark.parametrize("dtype,d,n_seq,hkv,G,kv,top,fused", [
+    ("bf16", 64, 32, 8, 4, 6500, 20, True),               # 256 lists of 407 candidates, one kernel
+    ("bf16", 128, 80, 4, 2, 6399, 8, True),
+    ("fp32", 64, 65, 4, 1, 7000, 40, True),
+    ("bf16", 256, 32, 8, 3, 6401, 9, True),
+    ("bf16", 64, 32, 8, 4, 6000, 20, False),              # 375 candidates: through scratch
+    ("bf16", 128, 100, 8, 1, 300, 7, False),              # many short lists
+    ("bf16", 64, 30, 8, 2, 9000, 33, False),              # 240 lists
+])
+def test_select_for_batches_of_single_tokens(dtype, d, n_seq, hkv, G, kv, top, fused):
+    import numpy as np
+    import paper_2601_17702_amd as s3
+    pr = paged.Problem(28 + kv, dtype, d, 16, hkv * G, hkv, [1] * n_seq, [1] * n_seq, spare=600 - n_seq)
+    pr.kv = [kv - 7 * s for s in range(n_seq)] if n_seq < 40 else [kv] * n_seq       # lengths that the pages below stand for
+    nb = -(-kv // 16)
+    pr.table = torch.randint(0, pr.n_pages, (n_seq, nb), generator=pr.g, dtype=torch.int32)
+    pr.table[:, 5] = -1
+    sig = torch.from_numpy(paged.grid8(torch.randn(pr.n_pages, hkv, d, generator=pr.g).numpy())).to(torch.bfloat16)
+    c = s3.KVCache(pr.n_pages, 16, hkv, d, pr.dtype, sig=sig.cuda())
+    kv_len, table = torch.tensor(pr.kv, dtype=torch.int32, device="cuda"), pr.table.cuda()
+    b = c._batch(n_seq, kv_len, table, None, 1, kv)
+    assert (s3.lib().s3_block_select_workspace(c._c, b, hkv * G, 1, top) == 0) == fused
+    sel = c.select(pr.q.cuda(), kv_len, table, top, lead=2, tail=1, max_kv=kv)
+    assert np.array_equal(sel.cpu().numpy(), paged.select(pr, sig, top, 1, 2, 1))
