@@ -451,17 +451,24 @@ int launch(const AttnArgs& p, int64_t tiles, int R, float* ws, hipStream_t st) {
     return S3_OK;
 }
 
+// Row sets of 32 as R needs them, as many as s3_few_rows lets through.
+template <typename T, int D, bool LIST>
+int launch_rows(const AttnArgs& p, int64_t tiles, int R, float* ws, hipStream_t st) {
+    constexpr int most = s3_few_rows(sizeof(T) == 2, D, LIST);
+    if constexpr (most > 64)
+        if (R > 64) return launch<T, D, LIST, 4>(p, tiles, R, ws, st);
+    if constexpr (most > 32)
+        if (R > 32) return launch<T, D, LIST, 2>(p, tiles, R, ws, st);
+    return launch<T, D, LIST, 1>(p, tiles, R, ws, st);
+}
+
 }  // namespace
 
 size_t s3_attn_stream_workspace(int d_head, int R) { return s3_align((size_t)kRunGroups * 2 * slot_floats(R, d_head) * 4); }
 
 int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st) {
-    const int rt = R <= 32 ? 1 : R <= 64 ? 2 : 4;
-#define S3_STREAM2(T, D, L) \
-    (rt == 1 ? launch<T, D, L, 1>(p, tiles, R, (float*)ws, st) : rt == 2 ? launch<T, D, L, 2>(p, tiles, R, (float*)ws, st) : launch<T, D, L, 4>(p, tiles, R, (float*)ws, st))
-#define S3_STREAM(T, D) (p.sel ? S3_STREAM2(T, D, true) : S3_STREAM2(T, D, false))
+#define S3_STREAM(T, D) (p.sel ? launch_rows<T, D, true>(p, tiles, R, (float*)ws, st) : launch_rows<T, D, false>(p, tiles, R, (float*)ws, st))
     if (c->dtype == S3_BF16) return c->d_head == 64 ? S3_STREAM(__bf16, 64) : c->d_head == 128 ? S3_STREAM(__bf16, 128) : S3_STREAM(__bf16, 256);
     return c->d_head == 64 ? S3_STREAM(float, 64) : c->d_head == 128 ? S3_STREAM(float, 128) : S3_STREAM(float, 256);
 #undef S3_STREAM
-#undef S3_STREAM2
 }

@@ -20,16 +20,6 @@ int check_ws(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
     return S3_OK;
 }
 
-// The most rows of one sequence (or tile of listed blocks) that the streaming kernel takes; the tiled kernel has more, whose 256 rows a
-// workgroup would stand mostly empty below.  us in the tiled / in the streaming kernel, 32 query heads over 8: 16 tokens of one sequence at
-// 32768 with d_head 64: 42 / 27, of eight at 8000 with 256: 258 / 208, in fp32: 355 / 217 (32 tokens: 579 / 375); tiles of 16
-// queries over 64 listed blocks of 512: 343 / 240, d_head 64: 276 / 154.  But bf16 with d_head 128, eight sequences: 66 / 73, where the tiled
-// kernel's rate is best.
-int few_rows(const s3_kv_cache* c, bool list) {
-    if (c->dtype == S3_FP32) return c->d_head == 128 ? 128 : 64;
-    return list || c->d_head != 128 ? 64 : 32;
-}
-
 // How a call is shared out.
 struct Plan {
     int G, R, qb, per_q, n_split, limit;
@@ -39,13 +29,13 @@ struct Plan {
     size_t bytes() const { return few_ws + many_ws; }
     Plan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b, int window) {
         G = n_q / c->n_kv_heads;
-        limit = few_rows(c, q_block != 0);
+        limit = s3_few_rows(c->dtype == S3_BF16, c->d_head, q_block != 0);
         qb = min(q_block, max(b->n_tokens, 1));
         const int most_new = min(max(b->max_new, 1), max(b->n_tokens, 1));
         const int64_t most = (int64_t)(q_block ? min(qb, most_new) : most_new) * G;
         many = most > limit;
         // Beside chunks up to 32 rows: more of them fill what the chunk leaves idle or not, by lengths that the host does not know.  us with 32 / with
-        // few_rows, 8 sequences of 16 tokens beside 512 at 2048: at 1000 tokens with d_head 256 139 / 200, in fp32 with 128 296 / 358, with 256 726 / 872; at 8000
+        // s3_few_rows, 8 sequences of 16 tokens beside 512 at 2048: at 1000 tokens with d_head 256 139 / 200, in fp32 with 128 296 / 358, with 256 726 / 872; at 8000
         // 577 / 357, 537 / 544, 1419 / 1021.
         if (many && !q_block) limit = 32;
         // no sequence is a short one if even the others at their longest leave more rows for it
