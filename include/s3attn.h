@@ -443,6 +443,81 @@ int s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const
                        int64_t q_tok_stride, int64_t q_head_stride, const int32_t* sel, int q_block, int top_b,
                        float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * The same cache in 8 bits, and what stands beside both: head norms on the way in, capped scores, tokens read back.
+ *
+ * An 8-bit cache holds rows of bf16.  An element is an e4m3 value (OCP: 4 significant bits, largest 448, one NaN for each sign) times a
+ * power of two that its token and head have, one for the key and one for the value:
+ *   k      [n_pages][n_kv_heads][d_head / 16][page_size][16]   e4m3
+ *   v      [n_pages][n_kv_heads][page_size / 16][d_head][16]   e4m3
+ *   scale  [n_pages][n_kv_heads][2][page_size]                 uint8: codes of the keys, then of the values; c stands for 2^(c - 127)
+ *   sig    as in s3_kv_cache, or NULL
+ * all 256-byte aligned.  Codes go from 1 to 247; others count as the nearer of the two.  What an element stands for is exact in bf16, 2^-126
+ * and more of it.  Limits as s3_kv_cache.
+ * Calls take such a cache where their name begins with s3_kv8_; rows that they take and give are bf16.  s3_block_select reads signatures only: give it
+ * an s3_kv_cache of S3_BF16 with the same k, v, sig and sizes. */
+typedef struct {
+    void* k;
+    void* v;
+    void* scale;
+    void* sig;
+    int n_pages, page_size, n_kv_heads, d_head;
+} s3_kv8_cache;
+
+/* Norms of queries and keys, before their rotation: y = (x r) w, with r = 1 / sqrt(sum x^2 / d_head + eps) of the row, the sum and the
+ * root in 64 bits and r rounded to fp32 once, both products rounded to fp32; the rotation goes on from there, and the result is rounded once.
+ *   q, k   fp32 weights [heads][d_head] (16-byte aligned; head strides in elements, multiples of 4; 0: the same for all heads), or NULL: no norm
+ * eps > 0.  A row with an infinite element has r = 0. */
+typedef struct {
+    const float* q;
+    const float* k;
+    int64_t q_head_stride, k_head_stride;
+    float eps;
+} s3_kv_norm;
+
+/* s3_kv_append with norms (norm: host, not NULL). */
+int s3_kv_append_norm(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* k, int64_t k_tok_stride,
+                      int64_t k_head_stride, const void* v, int64_t v_tok_stride, int64_t v_head_stride, const float* rope,
+                      int64_t n_pos, int rot_dim, int interleaved, const int32_t* positions, const void* q, int n_q_heads,
+                      int64_t q_tok_stride, int64_t q_head_stride, void* q_out, const s3_kv_norm* norm, void* stream);
+
+/* s3_kv_append to an 8-bit cache (norm may be NULL); k, v, q and q_out are bf16.  A row's code is the smallest c >= 1 that leaves no finite
+ * |x| 2^(127 - c) above 448, x the fp32 values after norm and rotation; its elements are x 2^(127 - c) rounded to e4m3, to nearest even.
+ * What is not finite is stored as NaN.  Signatures are of the keys as they are stored. */
+int s3_kv8_append(const s3_kv8_cache* cache, const s3_kv_batch* batch, const void* k, int64_t k_tok_stride,
+                  int64_t k_head_stride, const void* v, int64_t v_tok_stride, int64_t v_head_stride, const float* rope,
+                  int64_t n_pos, int rot_dim, int interleaved, const int32_t* positions, const void* q, int n_q_heads,
+                  int64_t q_tok_stride, int64_t q_head_stride, void* q_out, const s3_kv_norm* norm, void* stream);
+
+/* s3_paged_attention and s3_block_attention with capped scores: softmax over softcap * tanh(scale q . k / softcap), lse of these.
+ * Masks hide a token from the softmax, whatever the cap.  0 < softcap <= 1e30, scale / softcap from 1e-30 to 1e30; workspaces as theirs.  A score is within 2^-20 of its magnitude. */
+int s3_paged_attention_capped(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
+                              int64_t q_tok_stride, int64_t q_head_stride, float scale, float softcap, int window, void* out,
+                              float* lse, void* ws, size_t ws_bytes, void* stream);
+int s3_block_attention_capped(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
+                              int64_t q_tok_stride, int64_t q_head_stride, const int32_t* sel, int q_block, int top_b,
+                              float scale, float softcap, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* s3_paged_attention and s3_block_attention over an 8-bit cache; q and out are bf16.  softcap as above, or 0: none.  Keys and values enter as what
+ * they stand for, exactly; the weights are rounded to bf16, as over a bf16 cache. */
+size_t s3_kv8_attention_workspace(const s3_kv8_cache* cache, const s3_kv_batch* batch, int n_q_heads);
+int s3_kv8_attention(const s3_kv8_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
+                     int64_t q_tok_stride, int64_t q_head_stride, float scale, float softcap, int window, void* out, float* lse,
+                     void* ws, size_t ws_bytes, void* stream);
+size_t s3_kv8_block_attention_workspace(const s3_kv8_cache* cache, const s3_kv_batch* batch, int n_q_heads, int q_block, int top_b);
+int s3_kv8_block_attention(const s3_kv8_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
+                           int64_t q_tok_stride, int64_t q_head_stride, const int32_t* sel, int q_block, int top_b, float scale,
+                           float softcap, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Tokens of the cache back as rows: row q_start[s] + i of the call is the token at positions[q_start[s] + i] of sequence s, or without
+ * positions the one that s3_kv_append would store from that row.
+ *   positions   [n_tokens] int32 or NULL
+ *   k_out, v_out  [n_tokens][n_kv_heads][d_head], contiguous, 16-byte aligned, dtype (8 bits: bf16, rounded to nearest even where 2^-126 is not reached); either may be NULL
+ * Positions outside [0, kv_len) and unmapped ones give rows of zeros; rows of no sequence are not written.
+ * Limits: n_tokens * n_kv_heads * d_head < 2^37. */
+int s3_kv_read(const s3_kv_cache* cache, const s3_kv_batch* batch, const int32_t* positions, void* k_out, void* v_out, void* stream);
+int s3_kv8_read(const s3_kv8_cache* cache, const s3_kv_batch* batch, const int32_t* positions, void* k_out, void* v_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,7 @@ class S3Error(RuntimeError):
 # s3_kv_cache and s3_kv_batch of the header, packed into bytes (a call takes their address; a ctypes structure takes four times
 # as long to fill)
 _KV_CACHE, _KV_BATCH = struct.Struct("PPPiiiii4x"), struct.Struct("PPPqiiiii4x")
+_KV8_CACHE, _KV_NORM = struct.Struct("PPPPiiii"), struct.Struct("PPqqf4x")         # s3_kv8_cache, s3_kv_norm
 
 
 def lib():
@@ -114,6 +115,18 @@ def lib():
         L.s3_block_attention_workspace.restype = sz
         L.s3_block_attention.argtypes = [vp, vp, vp, ci, i64, i64, vp, ci, ci, cf, vp, vp, vp, sz, vp]
         L.s3_block_attention.restype = ci
+        for name in ("s3_kv_append_norm", "s3_kv8_append"):
+            getattr(L, name).argtypes = [vp, vp, vp, i64, i64, vp, i64, i64, vp, i64, ci, ci, vp, vp, ci, i64, i64, vp, vp, vp]
+        for name in ("s3_paged_attention_capped", "s3_kv8_attention"):
+            getattr(L, name).argtypes = [vp, vp, vp, ci, i64, i64, cf, cf, ci, vp, vp, vp, sz, vp]
+        for name in ("s3_block_attention_capped", "s3_kv8_block_attention"):
+            getattr(L, name).argtypes = [vp, vp, vp, ci, i64, i64, vp, ci, ci, cf, cf, vp, vp, vp, sz, vp]
+        for name in ("s3_kv_read", "s3_kv8_read"):
+            getattr(L, name).argtypes = [vp, vp, vp, vp, vp, vp]
+        L.s3_kv8_attention_workspace.argtypes = [vp, vp, ci]
+        L.s3_kv8_attention_workspace.restype = sz
+        L.s3_kv8_block_attention_workspace.argtypes = [vp, vp, ci, ci, ci]
+        L.s3_kv8_block_attention_workspace.restype = sz
         for name in ("s3_sae_encode_topk", "s3_sae_encode_topk_stream", "s3_index_create", "s3_index_append", "s3_index_finalize",
                      "s3_index_csr", "s3_index_build", "s3_coactivate_score"):
             getattr(L, name).restype = ci
@@ -510,7 +523,7 @@ class KVCache:
         lib()
         self.scale = d_head ** -0.5
         self.dtype, self.page_size, self.n_kv_heads, self.d_head, self.n_pages = dtype, page_size, n_kv_heads, d_head, n_pages
-        self._c = _KV_CACHE.pack(_ptr(self.k), _ptr(self.v), _ptr(self.sig) or 0, _dtype_code(self.k), n_pages, page_size, n_kv_heads, d_head)
+        self._c = self._c16 = _KV_CACHE.pack(_ptr(self.k), _ptr(self.v), _ptr(self.sig) or 0, _dtype_code(self.k), n_pages, page_size, n_kv_heads, d_head)
 
     # These run before every launch: as few attribute reads as the checks allow.
     def _batch(self, n_tokens, kv_len, block_table, q_start, max_new, max_kv):
@@ -536,10 +549,18 @@ class KVCache:
         assert x.dtype is self.dtype and x.is_cuda and d == self.d_head and inner == 1 and (heads is None or n == heads)
         return x.data_ptr(), ts, hs
 
+    def _weights(self, w, heads):
+        """A norm's weights, [d_head] for all heads or [heads, d_head]: address, and from head to head."""
+        if w is None:
+            return 0, 0
+        assert w.is_cuda and w.dtype is _torch().float32 and w.is_contiguous() and w.shape in ((self.d_head,), (heads, self.d_head))
+        return w.data_ptr(), self.d_head if w.dim() == 2 else 0
+
     def append(self, k, v, kv_len, block_table, q_start=None, rope=None, interleaved: bool = False, positions=None, q=None, q_out=None,
-               max_new=None):
-        """s3_kv_append: k, v [n_tokens, n_kv_heads, d_head] into their pages, keys (and q) rotated by rope (rope_table) first.
-        Returns the rotated q, or None without q."""
+               max_new=None, q_norm=None, k_norm=None, eps: float = 1e-6):
+        """s3_kv_append: k, v [n_tokens, n_kv_heads, d_head] into their pages, keys (and q) rotated by rope (rope_table) first.  With q_norm
+        or k_norm (fp32 weights, [d_head] or [heads, d_head]) s3_kv_append_norm: rows over the root of their mean square plus eps, before the
+        rotation.  Returns the rotated q, or None without q."""
         T = k.shape[0]
         kp, kt, kh = self._rows(k, self.n_kv_heads)
         vp, vt, vh = self._rows(v, self.n_kv_heads)
@@ -560,10 +581,39 @@ class KVCache:
                 q_out = _torch().empty_like(q, memory_format=_torch().contiguous_format)
             assert q_out.shape == q.shape and q_out.dtype is q.dtype and q_out.is_contiguous() and q_out.is_cuda
             op = q_out.data_ptr()
-        rc = _lib.s3_kv_append(self._c, b, kp, kt, kh, vp, vt, vh, rp, n_pos, rot, interleaved, _ptr(positions), qp, n_q, qt, qh, op, _stream())
+        norm = None
+        if q_norm is not None or k_norm is not None:
+            assert q_norm is None or q is not None
+            (qw, qs), (kw, ks) = self._weights(q_norm, n_q), self._weights(k_norm, self.n_kv_heads)
+            norm = _KV_NORM.pack(qw, kw, qs, ks, eps)
+        rc = self._append((self._c, b, kp, kt, kh, vp, vt, vh, rp, n_pos, rot, interleaved, _ptr(positions), qp, n_q, qt, qh, op), norm)
         if rc:
             _check(rc)
         return q_out
+
+    @staticmethod
+    def _append(args, norm):
+        return _lib.s3_kv_append(*args, _stream()) if norm is None else _lib.s3_kv_append_norm(*args, norm, _stream())
+
+    def read(self, kv_len, block_table, n_rows: int, q_start=None, positions=None, k_out=None, v_out=None):
+        """s3_kv_read: tokens back as rows.  Rows q_start[s] .. q_start[s + 1] - 1 (None: row s) are those of sequence s at `positions`
+        [n_rows] int32, or without them its last ones, as append would store them.  Returns (k, v) [n_rows, n_kv_heads, d_head]."""
+        torch = _torch()
+        b = self._batch(n_rows, kv_len, block_table, q_start, None, None)
+        if positions is not None:
+            assert positions.is_cuda and positions.is_contiguous() and positions.dtype is torch.int32 and positions.shape == (n_rows,)
+        shape = (n_rows, self.n_kv_heads, self.d_head)
+        k, v = (kv_len.new_empty(shape, dtype=self.dtype) if x is None else x for x in (k_out, v_out))
+        for x in (k, v):
+            assert x.is_cuda and x.is_contiguous() and x.dtype is self.dtype and x.shape == shape
+        rc = self._read(self._c, b, _ptr(positions), k.data_ptr(), v.data_ptr(), _stream())
+        if rc:
+            _check(rc)
+        return k, v
+
+    @staticmethod
+    def _read(*args):
+        return _lib.s3_kv_read(*args)
 
     @staticmethod
     def _scratch(q, need, ws):
@@ -581,17 +631,33 @@ class KVCache:
         lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
         return out, lse, self._scratch(q, need, ws)
 
+    def _attend(self, head, scale, softcap, window, tail):
+        if softcap:
+            return _lib.s3_paged_attention_capped(*head, scale, softcap, window, *tail)
+        return _lib.s3_paged_attention(*head, scale, window, *tail)
+
+    def _attend_blocks(self, head, scale, softcap, tail):
+        if softcap:
+            return _lib.s3_block_attention_capped(*head, scale, softcap, *tail)
+        return _lib.s3_block_attention(*head, scale, *tail)
+
+    def _attend_workspace(self, *args):
+        return _lib.s3_paged_attention_workspace(*args)
+
+    def _attend_blocks_workspace(self, *args):
+        return _lib.s3_block_attention_workspace(*args)
+
     def attention(self, q, kv_len, block_table, q_start=None, scale=None, window: int = 0, max_new=None, max_kv=None, out=None,
-                  want_lse: bool = False, ws=None):
-        """s3_paged_attention: q [n_tokens, n_q_heads, d_head] over all that the sequences hold (append first).  Returns
-        (out, lse fp32 [n_tokens, n_q_heads] | None)."""
+                  want_lse: bool = False, ws=None, softcap: float = 0.0):
+        """s3_paged_attention: q [n_tokens, n_q_heads, d_head] over all that the sequences hold (append first); with softcap
+        s3_paged_attention_capped: scores softcap * tanh(score / softcap).  Returns (out, lse fp32 [n_tokens, n_q_heads] | None)."""
         T, n_q, _ = q.shape
         b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
         qp, qt, qh = self._rows(q)
-        need = _lib.s3_paged_attention_workspace(self._c, b, n_q)
+        need = self._attend_workspace(self._c, b, n_q)
         out, lse, ws = self._out(q, out, want_lse, need, ws)
-        rc = _lib.s3_paged_attention(self._c, b, qp, n_q, qt, qh, self.scale if scale is None else scale, window, out.data_ptr(),
-                                     _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+        rc = self._attend((self._c, b, qp, n_q, qt, qh), self.scale if scale is None else scale, softcap, window,
+                          (out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
         if rc:
             _check(rc)
         return out, lse
@@ -605,17 +671,17 @@ class KVCache:
         b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
         qp, qt, qh = self._rows(q)
         sel = q.new_empty((_lib.s3_block_tiles(b, q_block), self.n_kv_heads, top_b), dtype=torch.int32)
-        need = _lib.s3_block_select_workspace(self._c, b, n_q, q_block, top_b)
+        need = _lib.s3_block_select_workspace(self._c16, b, n_q, q_block, top_b)
         ws = self._scratch(q, need, ws)
-        rc = _lib.s3_block_select(self._c, b, qp, n_q, qt, qh, q_block, top_b, lead, tail, sel.data_ptr(), _ptr(ws),
+        rc = _lib.s3_block_select(self._c16, b, qp, n_q, qt, qh, q_block, top_b, lead, tail, sel.data_ptr(), _ptr(ws),
                                   0 if ws is None else ws.numel(), _stream())
         if rc:
             _check(rc)
         return sel
 
     def block_attention(self, q, kv_len, block_table, sel, q_start=None, q_block: int = 1, scale=None, max_new=None, max_kv=None,
-                        out=None, want_lse: bool = False, ws=None):
-        """s3_block_attention: as attention, over the blocks that sel [tiles, n_kv_heads, top_b] lists (select, or blocks of
+                        out=None, want_lse: bool = False, ws=None, softcap: float = 0.0):
+        """s3_block_attention (softcap: s3_block_attention_capped): as attention, over the blocks that sel [tiles, n_kv_heads, top_b] lists (select, or blocks of
         evidence spans).  Returns (out, lse | None)."""
         T, n_q, _ = q.shape
         b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
@@ -623,10 +689,57 @@ class KVCache:
         tiles, heads, top_b = sel.shape
         assert sel.is_cuda and sel.is_contiguous() and sel.dtype is kv_len.dtype and heads == self.n_kv_heads
         assert tiles >= _lib.s3_block_tiles(b, q_block)
-        need = _lib.s3_block_attention_workspace(self._c, b, n_q, q_block, top_b)
+        need = self._attend_blocks_workspace(self._c, b, n_q, q_block, top_b)
         out, lse, ws = self._out(q, out, want_lse, need, ws)
-        rc = _lib.s3_block_attention(self._c, b, qp, n_q, qt, qh, sel.data_ptr(), q_block, top_b, self.scale if scale is None else scale,
-                                     out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+        rc = self._attend_blocks((self._c, b, qp, n_q, qt, qh, sel.data_ptr(), q_block, top_b), self.scale if scale is None else scale, softcap,
+                                 (out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
         if rc:
             _check(rc)
         return out, lse
+
+
+class KVCache8(KVCache):
+    """The same in 8 bits (s3_kv8_cache): half of a bf16 cache's memory, and of its traffic.  k [n_pages, n_kv_heads, d_head / 16, page_size, 16] and
+    v [n_pages, n_kv_heads, page_size / 16, d_head, 16] in float8_e4m3fn, scale [n_pages, n_kv_heads, 2, page_size] uint8: element times
+    2^(code - 127) is what it stands for.  Every call of KVCache is here, with the same arguments; rows are bfloat16."""
+
+    def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, signatures: bool = False, device="cuda", k=None, v=None,
+                 scale=None, sig=None):
+        import torch
+        f8 = torch.float8_e4m3fn
+
+        def array(name, t, dt, shape):
+            if t is None:
+                return torch.empty(shape, dtype=dt, device=device)
+            assert t.is_cuda and t.is_contiguous() and t.dtype == dt and tuple(t.shape) == shape, name
+            return t
+        self.k = array("k", k, f8, (n_pages, n_kv_heads, d_head // 16, page_size, 16))
+        self.v = array("v", v, f8, (n_pages, n_kv_heads, page_size // 16, d_head, 16))
+        self.codes = array("scale", scale, torch.uint8, (n_pages, n_kv_heads, 2, page_size))
+        self.sig = array("sig", sig, torch.bfloat16, (n_pages, n_kv_heads, d_head)) if signatures or sig is not None else None
+        lib()
+        self.scale = d_head ** -0.5
+        self.dtype, self.page_size, self.n_kv_heads, self.d_head, self.n_pages = torch.bfloat16, page_size, n_kv_heads, d_head, n_pages
+        sizes = (n_pages, page_size, n_kv_heads, d_head)
+        self._c = _KV8_CACHE.pack(_ptr(self.k), _ptr(self.v), _ptr(self.codes), _ptr(self.sig) or 0, *sizes)
+        self._c16 = _KV_CACHE.pack(_ptr(self.k), _ptr(self.v), _ptr(self.sig) or 0, S3_BF16, *sizes)      # for the choice, which reads sig only
+
+    @staticmethod
+    def _append(args, norm):
+        return _lib.s3_kv8_append(*args, norm, _stream())
+
+    @staticmethod
+    def _read(*args):
+        return _lib.s3_kv8_read(*args)
+
+    def _attend(self, head, scale, softcap, window, tail):
+        return _lib.s3_kv8_attention(*head, scale, softcap, window, *tail)
+
+    def _attend_blocks(self, head, scale, softcap, tail):
+        return _lib.s3_kv8_block_attention(*head, scale, softcap, *tail)
+
+    def _attend_workspace(self, *args):
+        return _lib.s3_kv8_attention_workspace(*args)
+
+    def _attend_blocks_workspace(self, *args):
+        return _lib.s3_kv8_block_attention_workspace(*args)

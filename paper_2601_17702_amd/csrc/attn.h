@@ -10,9 +10,10 @@
 template <int D, typename T> constexpr int kQSteps = D * (int)sizeof(T) / 32;       // 16-byte pieces of a row per lane
 
 // Token of the 32 in row m of the first product's tile.
-template <typename T>
+template <typename S>
 __device__ __forceinline__ int kv_token(int m) {
-    if constexpr (KvElem<T>::E == 8) return (m & 0x13) | ((m & 4) << 1) | ((m & 8) >> 1);
+    if constexpr (KvStore<S>::E == 16) return (m & 4) << 2 | (m & 0x18) >> 1 | (m & 3);
+    else if constexpr (KvStore<S>::E == 8) return (m & 0x13) | ((m & 4) << 1) | ((m & 8) >> 1);
     else return m;
 }
 
@@ -32,11 +33,13 @@ struct AttnArgs {
     float* lse;
     const char* k;
     const char* v;
+    const uint8_t* scale;     // an 8-bit cache's
     const int32_t* sel;       // block lists, or null: all blocks
     int64_t q_ts, q_hs;       // bytes
     int n_kv, G, n_q, window;
     int qb, top, per_q, lists;// lists: tokens a tile, entries, row tiles a tile of queries (tiled kernel), how many lists there are
-    float sl;                 // scale * log2(e)
+    float sl;                 // scale * log2(e); 1 with a cap, whose scores come scaled
+    float cap, to_cap;        // cap * log2(e), or 0: none; scale / cap
     int few;                  // sequences of at most this many rows are the streaming kernel's
 };
 
@@ -51,7 +54,8 @@ __device__ __forceinline__ float kv_pair_sum(float x) {
 }
 
 // What a wavefront knows of its 32 rows: row r0 + (lane & 31) of the sequence's n * G, head and token of it.
-template <typename T, int D>
+// An 8-bit cache's pieces hold 16 channels, which two instructions take: this lane's 8 of either lie side by side.
+template <typename T, int D, bool SIDE_BY_SIDE = false>
 struct AttnRows {
     typename KvElem<T>::vec q[kQSteps<D, T>];
     int64_t row;              // token * n_q + head, or -1
@@ -65,9 +69,9 @@ struct AttnRows {
             const int t = r / p.G, g = r - t * p.G;
             row = (int64_t)(first + t) * p.n_q + head * p.G + g;
             pos = max(len - n + t, -1);
-            const char* src = p.q + (int64_t)(first + t) * p.q_ts + (int64_t)(head * p.G + g) * p.q_hs + half * 16;
+            const char* src = p.q + (int64_t)(first + t) * p.q_ts + (int64_t)(head * p.G + g) * p.q_hs + half * (SIDE_BY_SIDE ? 32 : 16);
 #pragma unroll
-            for (int s = 0; s < kQSteps<D, T>; ++s) q[s] = *(const typename KvElem<T>::vec*)(src + s * 32);
+            for (int s = 0; s < kQSteps<D, T>; ++s) q[s] = *(const typename KvElem<T>::vec*)(src + (SIDE_BY_SIDE ? s / 2 * 64 + s % 2 * 16 : s * 32));
         } else {
 #pragma unroll
             for (int s = 0; s < kQSteps<D, T>; ++s) q[s] = zero;
@@ -88,7 +92,17 @@ __device__ __forceinline__ unsigned kv_magnitude(kv_f32x4 v, unsigned x) {
     for (int i = 0; i < 4; ++i) x = max(x, u[i] & 0x7fffffffu);
     return x;
 }
+__device__ __forceinline__ unsigned kv_magnitude(kv_u32x4 u, unsigned x) {       // e4m3: a NaN is the only such
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x |= (((u[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) ? 0x7f800000u : 0u;
+    return x;
+}
 // Zero in place of infinities and NaN.
+__device__ __forceinline__ kv_u32x4 kv_finite(kv_u32x4 u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] &= ~(((((u[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u);
+    return u;
+}
 __device__ __forceinline__ kv_bf16x8 kv_finite(kv_bf16x8 v) {
     kv_u32x4 u = __builtin_bit_cast(kv_u32x4, v);
 #pragma unroll
@@ -116,6 +130,12 @@ __device__ __forceinline__ kv_f32x4 kv_first(kv_f32x4 v, int n) {
     return v;
 }
 
+__device__ __forceinline__ kv_u32x4 kv_first(kv_u32x4 u, int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] &= n >= 4 * i + 4 ? ~0u : n > 4 * i ? (1u << (n - 4 * i) * 8) - 1u : 0u;
+    return u;
+}
+
 // The tokens a row sees, as low <= position <= low + span; position 2^30 is beyond all rows.
 struct AttnSight {
     int low;
@@ -136,11 +156,13 @@ struct AttnSight {
 // far, -inf before there is one; l this lane's part of the weights' sum, o the products so far: o[dt][i] is channel 32 dt + 8 (i / 4) + 4 half + i % 4.
 // Rescaling o takes D / 2 instructions per 32 tokens, more than the exponentials: it is done only where a row's largest score has
 // grown by more than kSlack (weights of up to 2^kSlack are as exact as those below 1).
-constexpr float kSlack = 8.0f, kLowest = -3.402823466e38f;
-template <typename T, int D>
+// SCALED: weights are multiplied by their tokens' scales, at most 2^120, before bf16 holds them: 2^127 at most so.
+constexpr float kLowest = -3.402823466e38f;
+template <typename T, int D, bool SCALED = false>
 struct AttnState {
     typedef typename KvElem<T>::vec vec;
     static constexpr int E = KvElem<T>::E, NW = 16 / E;
+    static constexpr float kSlack = SCALED ? 7.0f : 8.0f;
     float m, l;
     kv_f32x16 o[D / 32];
     __device__ __forceinline__ void clear() {
@@ -187,6 +209,19 @@ struct AttnState {
         asm volatile("" : "+v"(l));      // summed here, not behind the products: nothing else would run beside it there
         return w;
     }
+    // The same of an 8-bit cache's 8 tokens, times what their values are to be scaled by (codes: a byte each): a power of two, so that nothing
+    // more is rounded, and one multiplication a weight in place of one for each of a token's values.
+    __device__ __forceinline__ vec weights(const kv_f32x16& s, int y, float sl, float sub, unsigned codes0, unsigned codes1) {
+        vec w;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float x = __builtin_amdgcn_exp2f(s[y * E + e] * sl - sub);
+            l += x;
+            w[e] = (T)(x * kv_scale((e < 4 ? codes0 : codes1) >> (e % 4 * 8)));
+        }
+        asm volatile("" : "+v"(l));
+        return w;
+    }
     // A token whose values are not all finite, in a tile where some rows do not see it: zero took the place of its infinities and NaNs
     // in the product (0 * inf is NaN), and the rows that do see it get them here.  value(c): the token's channel c.
     template <typename V>
@@ -202,6 +237,33 @@ struct AttnState {
             }
     }
 };
+
+// Capped scores: c tanh(z) for this lane's raw scores x, z = x u, c in log2 units.  Below |z| = 0.35 by tanh's series (its next term, 1382 z^11 / 155925, is
+// 2^-22 of z there), above as 1 - 2 / (1 + exp(2 z)), whose error of 2^-23 or so is relative to one.  Where all of a wavefront's are small, as a cap well above
+// the scores leaves them, only the series runs: 7 instructions a score; the exponential, the reciprocal and the choice are 44 cycles more.
+template <int N>
+__device__ __forceinline__ void kv_cap(kv_f32x16 (&s)[N], float u, float c) {
+    float most = 0.0f;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(s[x][i]));
+    const bool some = __ballot(!(most * u < 0.35f)) != 0;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float z = s[x][i] * u, w = z * z;
+            const float small = z * c * fmaf(w, fmaf(w, fmaf(w, fmaf(w, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+            if (some) {
+                const float t = __builtin_amdgcn_exp2f(z * 2.8853900817779268f);
+                const float large = fmaf(__builtin_amdgcn_rcpf(t + 1.0f), -2.0f * c, c);
+                s[x][i] = fabsf(z) < 0.35f ? small : large;
+            } else {
+                s[x][i] = small;
+            }
+        }
+}
 
 // 1 / l, or what makes a row that saw nothing 0 (infinity makes NaN of one that saw only scores of -inf); its lse.
 __device__ __forceinline__ float kv_inverse(float m, float l) { return m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l; }

@@ -14,9 +14,20 @@ constexpr int s3_few_rows(bool bf16, int d_head, bool list) {
 // Sequences, or tiles of listed blocks, of few rows (R: the most that one has, 128 at most); tiles: how many there can be.
 size_t s3_attn_stream_workspace(int d_head, int R);
 int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
+// Its builds for capped scores, for 8-bit caches (dtype kS3E4m3), and for both.
+int s3_attn_stream_cap(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
+int s3_attn_stream_8(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
+int s3_attn_stream_8_cap(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
 
 // Chunks, or tiles of listed blocks, of more rows: row tiles of s3_attn_tile_rows rows, the tokens of each in n_split parts.
 int s3_attn_tile_rows(const s3_kv_cache* c);
 int s3_attn_tile_split(const s3_kv_cache* c, int64_t units, int64_t tokens, bool ragged);
 size_t s3_attn_tile_workspace(const s3_kv_cache* c, int64_t units, int n_split);
+struct TileArgs {
+    float* slots;             // partial sums where n_split > 1
+    int n_split, tiles;       // row tiles that there can be
+};
 int s3_attn_tile(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int n_split, void* ws, hipStream_t st);
+int s3_attn_tile_cap(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);
+int s3_attn_tile_8(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);
+int s3_attn_tile_8_cap(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);

@@ -29,7 +29,7 @@ struct Plan {
     size_t bytes() const { return few_ws + many_ws; }
     Plan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b, int window) {
         G = n_q / c->n_kv_heads;
-        limit = s3_few_rows(c->dtype == S3_BF16, c->d_head, q_block != 0);
+        limit = s3_few_rows(c->dtype != S3_FP32, c->d_head, q_block != 0);
         qb = min(q_block, max(b->n_tokens, 1));
         const int most_new = min(max(b->max_new, 1), max(b->n_tokens, 1));
         const int64_t most = (int64_t)(q_block ? min(qb, most_new) : most_new) * G;
@@ -74,6 +74,47 @@ bool shapes_ok(const s3_kv_cache* c, const s3_kv_batch* b, int n_q) {
     return !s3_kv_check("workspace", c, b) && n_q >= 1 && n_q % c->n_kv_heads == 0 && n_q / c->n_kv_heads <= 32;
 }
 
+// An entry point's call.  c: the cache, or an 8-bit one (its scale) as one of bf16; softcap: 0 for none; sel: listed blocks, or null.
+struct Call {
+    const char* fn;
+    const s3_kv_cache* c;
+    const uint8_t* scale8;
+    const s3_kv_batch* b;
+    const void* q;
+    int n_q;
+    int64_t q_ts, q_hs;
+    float scale, softcap;
+    void* out;
+    float* lse;
+    void* ws;
+    size_t ws_bytes;
+    void* stream;
+};
+int attend(const Call& x, int window, const int32_t* sel, int q_block, int top_b) {
+    if (!(x.softcap >= 0.0f && x.softcap <= 1e30f)) return s3_fail(S3_EINVAL, "%s: softcap %g", x.fn, (double)x.softcap);
+    if (x.softcap > 0.0f && x.scale > 0.0f && !(x.scale / x.softcap >= 1e-30f && x.scale / x.softcap <= 1e30f))
+        return s3_fail(S3_EINVAL, "%s: scale %g over softcap %g", x.fn, (double)x.scale, (double)x.softcap);
+    if (int rc = check(x.fn, x.c, x.b, x.q, x.n_q, x.q_ts, x.q_hs, x.scale, x.out)) return rc < 0 ? rc : S3_OK;
+    if (q_block && !sel) return s3_fail(S3_EINVAL, "%s: null sel", x.fn);
+    if (window >= 1 << 30) window = 0;                        // no position is that far back: all of them, and none of the kernels' differences overflows
+    s3_kv_cache c = *x.c;
+    const int es = c.dtype == S3_BF16 ? 2 : 4;
+    if (x.scale8) c.dtype = kS3E4m3;
+    const Plan plan(&c, x.b, x.n_q, q_block, top_b, window);
+    if (int rc = check_ws(x.fn, x.ws, x.ws_bytes, plan.bytes())) return rc;
+    const float log2e = 1.4426950408889634f;
+    const bool cap = x.softcap > 0.0f;
+    const AttnArgs p{s3_kv_batch_args(&c, x.b), (const char*)x.q, (char*)x.out, x.lse, (const char*)c.k, (const char*)c.v, x.scale8, sel, x.q_ts * es,
+                     x.q_hs * es, c.n_kv_heads, plan.G, x.n_q, window, 0, top_b, 1, q_block ? (int)s3_block_tiles(x.b, q_block) : 0,
+                     cap ? 1.0f : x.scale * log2e, cap ? x.softcap * log2e : 0.0f, cap ? x.scale / x.softcap : 0.0f, 0};
+    return run(x.fn, &c, x.b, p, plan, x.ws, (hipStream_t)x.stream);
+}
+int check_window(const char* fn, int window) { return window < 0 ? s3_fail(S3_EINVAL, "%s: window %d", fn, window) : S3_OK; }
+int check_lists(const char* fn, int q_block, int top_b) {
+    return q_block < 1 || top_b < 1 || q_block > 1 << 20 || top_b > 4096 ? s3_fail(S3_EINVAL, "%s: q_block %d, top_b %d", fn, q_block, top_b) : S3_OK;
+}
+int check_cap(const char* fn, float softcap) { return softcap == 0.0f ? s3_fail(S3_EINVAL, "%s: softcap 0", fn) : S3_OK; }
+
 }  // namespace
 
 extern "C" size_t s3_paged_attention_workspace(const s3_kv_cache* c, const s3_kv_batch* b, int n_q) {
@@ -83,15 +124,16 @@ extern "C" size_t s3_paged_attention_workspace(const s3_kv_cache* c, const s3_kv
 extern "C" int s3_paged_attention(const s3_kv_cache* c, const s3_kv_batch* b, const void* q, int n_q, int64_t q_ts, int64_t q_hs,
                                   float scale, int window, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
     const char* fn = "s3_paged_attention";
-    if (window < 0) return s3_fail(S3_EINVAL, "%s: window %d", fn, window);
-    if (int rc = check(fn, c, b, q, n_q, q_ts, q_hs, scale, out)) return rc < 0 ? rc : S3_OK;
-    if (window >= 1 << 30) window = 0;                        // no position is that far back: all of them, and none of the kernels' differences overflows
-    const Plan plan(c, b, n_q, 0, 0, window);
-    if (int rc = check_ws(fn, ws, ws_bytes, plan.bytes())) return rc;
-    const int es = c->dtype == S3_BF16 ? 2 : 4;
-    AttnArgs p{s3_kv_batch_args(c, b), (const char*)q, (char*)out, lse, (const char*)c->k, (const char*)c->v, nullptr, q_ts * es,
-               q_hs * es, c->n_kv_heads, plan.G, n_q, window, 0, 0, 1, 0, scale * 1.4426950408889634f, 0};
-    return run(fn, c, b, p, plan, ws, (hipStream_t)stream);
+    if (int rc = check_window(fn, window)) return rc;
+    return attend({fn, c, nullptr, b, q, n_q, q_ts, q_hs, scale, 0.0f, out, lse, ws, ws_bytes, stream}, window, nullptr, 0, 0);
+}
+
+extern "C" int s3_paged_attention_capped(const s3_kv_cache* c, const s3_kv_batch* b, const void* q, int n_q, int64_t q_ts, int64_t q_hs,
+                                         float scale, float softcap, int window, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    const char* fn = "s3_paged_attention_capped";
+    if (int rc = check_window(fn, window)) return rc;
+    if (int rc = check_cap(fn, softcap)) return rc;
+    return attend({fn, c, nullptr, b, q, n_q, q_ts, q_hs, scale, softcap, out, lse, ws, ws_bytes, stream}, window, nullptr, 0, 0);
 }
 
 extern "C" int64_t s3_block_tiles(const s3_kv_batch* b, int q_block) {
@@ -106,13 +148,48 @@ extern "C" int s3_block_attention(const s3_kv_cache* c, const s3_kv_batch* b, co
                                   const int32_t* sel, int q_block, int top_b, float scale, void* out, float* lse, void* ws,
                                   size_t ws_bytes, void* stream) {
     const char* fn = "s3_block_attention";
-    if (q_block < 1 || top_b < 1 || q_block > 1 << 20 || top_b > 4096) return s3_fail(S3_EINVAL, "%s: q_block %d, top_b %d", fn, q_block, top_b);
-    if (int rc = check(fn, c, b, q, n_q, q_ts, q_hs, scale, out)) return rc < 0 ? rc : S3_OK;
-    if (!sel) return s3_fail(S3_EINVAL, "%s: null sel", fn);
-    const Plan plan(c, b, n_q, q_block, top_b, 0);
-    if (int rc = check_ws(fn, ws, ws_bytes, plan.bytes())) return rc;
-    const int es = c->dtype == S3_BF16 ? 2 : 4;
-    AttnArgs p{s3_kv_batch_args(c, b), (const char*)q, (char*)out, lse, (const char*)c->k, (const char*)c->v, sel, q_ts * es,
-               q_hs * es, c->n_kv_heads, plan.G, n_q, 0, 0, top_b, 1, (int)s3_block_tiles(b, q_block), scale * 1.4426950408889634f, 0};
-    return run(fn, c, b, p, plan, ws, (hipStream_t)stream);
+    if (int rc = check_lists(fn, q_block, top_b)) return rc;
+    return attend({fn, c, nullptr, b, q, n_q, q_ts, q_hs, scale, 0.0f, out, lse, ws, ws_bytes, stream}, 0, sel, q_block, top_b);
+}
+
+extern "C" int s3_block_attention_capped(const s3_kv_cache* c, const s3_kv_batch* b, const void* q, int n_q, int64_t q_ts, int64_t q_hs,
+                                         const int32_t* sel, int q_block, int top_b, float scale, float softcap, void* out, float* lse, void* ws,
+                                         size_t ws_bytes, void* stream) {
+    const char* fn = "s3_block_attention_capped";
+    if (int rc = check_lists(fn, q_block, top_b)) return rc;
+    if (int rc = check_cap(fn, softcap)) return rc;
+    return attend({fn, c, nullptr, b, q, n_q, q_ts, q_hs, scale, softcap, out, lse, ws, ws_bytes, stream}, 0, sel, q_block, top_b);
+}
+
+extern "C" size_t s3_kv8_attention_workspace(const s3_kv8_cache* c, const s3_kv_batch* b, int n_q) {
+    s3_kv_cache view;
+    if (s3_kv8_check("workspace", c, b, view) || !shapes_ok(&view, b, n_q)) return 0;
+    view.dtype = kS3E4m3;
+    return Plan(&view, b, n_q, 0, 0, 0).bytes();
+}
+
+extern "C" int s3_kv8_attention(const s3_kv8_cache* c, const s3_kv_batch* b, const void* q, int n_q, int64_t q_ts, int64_t q_hs,
+                                float scale, float softcap, int window, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    const char* fn = "s3_kv8_attention";
+    s3_kv_cache view;
+    if (int rc = s3_kv8_check(fn, c, b, view)) return rc;
+    if (int rc = check_window(fn, window)) return rc;
+    return attend({fn, &view, (const uint8_t*)c->scale, b, q, n_q, q_ts, q_hs, scale, softcap, out, lse, ws, ws_bytes, stream}, window, nullptr, 0, 0);
+}
+
+extern "C" size_t s3_kv8_block_attention_workspace(const s3_kv8_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b) {
+    s3_kv_cache view;
+    if (s3_kv8_check("workspace", c, b, view) || !shapes_ok(&view, b, n_q) || q_block < 1 || top_b < 1) return 0;
+    view.dtype = kS3E4m3;
+    return Plan(&view, b, n_q, q_block, top_b, 0).bytes();
+}
+
+extern "C" int s3_kv8_block_attention(const s3_kv8_cache* c, const s3_kv_batch* b, const void* q, int n_q, int64_t q_ts, int64_t q_hs,
+                                      const int32_t* sel, int q_block, int top_b, float scale, float softcap, void* out, float* lse, void* ws,
+                                      size_t ws_bytes, void* stream) {
+    const char* fn = "s3_kv8_block_attention";
+    s3_kv_cache view;
+    if (int rc = s3_kv8_check(fn, c, b, view)) return rc;
+    if (int rc = check_lists(fn, q_block, top_b)) return rc;
+    return attend({fn, &view, (const uint8_t*)c->scale, b, q, n_q, q_ts, q_hs, scale, softcap, out, lse, ws, ws_bytes, stream}, 0, sel, q_block, top_b);
 }

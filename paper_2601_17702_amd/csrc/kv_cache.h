@@ -19,6 +19,42 @@ template <> struct KvElem<float> {
     typedef kv_f32x4 vec;
 };
 
+// What a cache holds: S elements, E of them in 16 bytes, of rows of type `row`.  An 8-bit cache holds rows of bf16 as e4m3 values and one power of two for
+// each token and head: what an element stands for is exact in bf16.
+struct kv_e4m3 {
+    unsigned char bits;
+};
+template <typename S> struct KvStore {
+    static constexpr int E = KvElem<S>::E, BYTES = (int)sizeof(S);
+    static constexpr bool EIGHT = false;
+    typedef S row;
+    typedef typename KvElem<S>::vec vec;
+};
+template <> struct KvStore<kv_e4m3> {
+    static constexpr int E = 16, BYTES = 1;
+    static constexpr bool EIGHT = true;
+    typedef __bf16 row;
+    typedef kv_u32x4 vec;
+};
+constexpr int kS3E4m3 = 2;             // s3_kv_cache.dtype inside the library; no caller's
+
+// Code c of a scale: 2^(c - 127), for c from 1 to 247, all that an append writes; others count as the nearer of the two.
+__device__ __forceinline__ float kv_scale(unsigned code) { return __builtin_amdgcn_fmed3f(__uint_as_float((code & 255u) << 23), 0x1p-126f, 0x1p120f); }
+// The smallest code >= 1 that leaves nothing above 448, the largest e4m3 value: max_abs_bits are a finite float's.
+__device__ __forceinline__ unsigned kv_scale_code(unsigned max_abs_bits) {
+    return (unsigned)max((int)(max_abs_bits >> 23) - 8 + ((max_abs_bits & 0x7fffffu) > 0x600000u ? 1 : 0), 1);
+}
+// Two elements (the low or the high half of a word) as fp32, and as bf16 times a power of two.
+typedef __attribute__((ext_vector_type(2))) float kv_f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 kv_bf16x2;
+template <bool HI> __device__ __forceinline__ kv_f32x2 kv_of8(unsigned u) { return __builtin_amdgcn_cvt_pk_f32_fp8((int)u, HI); }
+// E 16 elements of one token: the first or the last 8 of them, times its scale.
+__device__ __forceinline__ kv_bf16x8 kv_of8_bf16(unsigned a, unsigned b, float scale) {
+    const kv_bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    const kv_bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+    return kv_bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
 // The sequences of a call, as the kernels read them.  Lengths and page numbers come from device memory, so every use is held
 // inside the arrays here: blocks to the table's width, tokens to n_tokens, pages to n_pages.
 struct KvBatch {
@@ -96,7 +132,8 @@ __device__ __forceinline__ float kv_grid(float x, int e) {      // multiples of 
     return rintf(x * __uint_as_float((unsigned)(127 - e) << 23)) * __uint_as_float((unsigned)(127 + e) << 23);
 }
 
-// Checks shared by the entry points (host).
+// Checks shared by the entry points (host).  s3_kv8_check: c as an s3_kv_cache of bf16 rows, for the checks and what else goes by shape.
+int s3_kv8_check(const char* fn, const s3_kv8_cache* c, const s3_kv_batch* b, s3_kv_cache& view);
 int s3_kv_check(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b);
 int s3_kv_check_rows(const char* fn, const char* what, const s3_kv_cache* c, const void* p, int64_t tok_stride, int64_t head_stride,
                      int heads);
