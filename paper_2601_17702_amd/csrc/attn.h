@@ -158,7 +158,9 @@ struct AttnSight {
 // grown by more than kSlack (weights of up to 2^kSlack are as exact as those below 1).
 // SCALED: weights are multiplied by their tokens' scales, at most 2^120, before bf16 holds them: 2^127 at most so.
 constexpr float kLowest = -3.402823466e38f;
-template <typename T, int D, bool SCALED = false>
+// PARTS: l takes E weights' sum at a time, as many additions, but an eighth of them to the long sum: 131072 tokens leave lse 1.2e-6 of itself off with one
+// at a time, 3e-7 so.
+template <typename T, int D, bool SCALED = false, bool PARTS = false>
 struct AttnState {
     typedef typename KvElem<T>::vec vec;
     static constexpr int E = KvElem<T>::E, NW = 16 / E;
@@ -200,12 +202,15 @@ struct AttnState {
     // outputs are then off by 2.0e-3 to 2.3e-3 of their norm, by 1.7e-3 with weights in fp32 (their own last rounding).
     __device__ __forceinline__ vec weights(const kv_f32x16& s, int y, float sl, float sub) {
         vec w;
+        float part = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float x = __builtin_amdgcn_exp2f(s[y * E + e] * sl - sub);
-            l += x;
+            if (PARTS) part = e ? part + x : x;
+            else l += x;
             w[e] = (T)x;
         }
+        if (PARTS) l += part;
         asm volatile("" : "+v"(l));      // summed here, not behind the products: nothing else would run beside it there
         return w;
     }
@@ -213,12 +218,14 @@ struct AttnState {
     // more is rounded, and one multiplication a weight in place of one for each of a token's values.
     __device__ __forceinline__ vec weights(const kv_f32x16& s, int y, float sl, float sub, unsigned codes0, unsigned codes1) {
         vec w;
+        float part = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float x = __builtin_amdgcn_exp2f(s[y * E + e] * sl - sub);
-            l += x;
+            part = e ? part + x : x;
             w[e] = (T)(x * kv_scale((e < 4 ? codes0 : codes1) >> (e % 4 * 8)));
         }
+        l += part;
         asm volatile("" : "+v"(l));
         return w;
     }

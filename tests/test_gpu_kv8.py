@@ -1,0 +1,508 @@
+"""GPU checks of the 8-bit cache and what stands beside it, against plain forms on the CPU (tests/paged8.py): head norms and quantising in the append,
+attention over 8 bits, capped scores, tokens read back."""
+import numpy as np
+import pytest
+import torch
+
+from tests import paged, paged8
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [   # d, P, hq, hkv, new, kv
+    (128, 64, 32, 8, [1], [1]),                               # the first token of all
+    (128, 64, 32, 8, [1, 1, 1], [63, 64, 65]),                # around a page's end
+    (128, 16, 28, 4, [5, 0, 33, 1], [5, 0, 40, 17]),          # seven query heads a head, a sequence without tokens
+    (64, 32, 8, 8, [70], [300]),                              # one query head a head
+    (256, 128, 16, 1, [3, 9], [129, 9]),                      # sixteen, wide heads
+    (128, 256, 32, 1, [2], [513]),                            # thirty-two
+    (64, 16, 4, 2, [130], [1000]),
+    (128, 64, 8, 2, [100, 1, 1, 7], [350, 1, 700, 7]),        # chunks beside single tokens
+    (256, 64, 4, 2, [150], [150]),                            # a whole prompt
+    (128, 64, 4, 1, [70], [9000]),                            # the tokens of a row tile in parts
+    (64, 64, 32, 1, [3, 1], [900, 40]),                       # 96 rows of three tokens
+    (256, 32, 3, 1, [1, 1], [3001, 33]),                      # an odd number of rows, in parts
+    (128, 16, 4, 1, [300], [301]),
+]
+
+
+def run(pr, c, **more):
+    kv_len, table = pr.args()
+    return c.attention(pr.q.cuda(), kv_len, table, q_start=pr.q_start.cuda(), want_lse=True, **more)
+
+
+@pytest.mark.parametrize("d,P,hq,hkv,new,kv", SHAPES)
+def test_attention(d, P, hq, hkv, new, kv):
+    pr = paged8.Problem8(len(kv) + d + P, d, P, hq, hkv, new, kv)
+    want, c = paged.attend(pr), pr.cache()
+    paged.check(pr, *run(pr, c), want)
+    o, lse = run(pr, c, max_new=max(new), max_kv=max(kv))
+    paged.check(pr, o, lse, want)
+    assert torch.equal(o, run(pr, c, max_new=max(new), max_kv=max(kv))[0])       # the same bits every time
+
+
+@pytest.mark.parametrize("d,P,hq,hkv,new,kv,window", [(128, 64, 8, 2, [1, 1], [500, 3], 100), (64, 16, 8, 2, [90], [400], 1),
+                                                      (128, 32, 4, 2, [100], [130], 33), (256, 16, 4, 2, [50, 1], [170, 90], 48)])
+def test_attention_window(d, P, hq, hkv, new, kv, window):
+    pr = paged8.Problem8(window + d, d, P, hq, hkv, new, kv)
+    paged.check(pr, *run(pr, pr.cache(), window=window), paged.attend(pr, window=window))
+
+
+@pytest.mark.parametrize("new,kv", [([10, 1], [4, 0]), ([200], [150]), ([1, 1], [0, 40])])
+def test_rows_that_see_nothing(new, kv):
+    pr = paged8.Problem8(1, 64, 16, 4, 2, new, kv)
+    want = paged.attend(pr)
+    assert torch.isinf(want[1]).any()
+    paged.check(pr, *run(pr, pr.cache()), want)
+
+
+@pytest.mark.parametrize("P,new", [(16, [1, 1]), (64, [50, 120]), (32, [2, 40])])
+def test_unmapped_pages_are_masked(P, new):
+    pr = paged8.Problem8(2, 128, P, 8, 2, new, [300, 310])
+    pr.table[0, 1] = -1
+    pr.table[1, 0] = pr.n_pages
+    pr.table[1, 2] = -(1 << 31)
+    pr.table[1, 300 // P] = (1 << 31) - 1
+    paged.check(pr, *run(pr, pr.cache()), paged.attend(pr))
+
+
+@pytest.mark.parametrize("d,new", [(64, 3), (128, 70), (256, 140), (128, 300), (64, 90)])
+def test_nan_reaches_only_rows_that_see_it(d, new):
+    pr = paged8.Problem8(3, d, 32, 4, 2, [new], [new + 50])
+    n = new + 50
+    for name, rows, (p, h, c) in (("v", pr.rows_v, (n - 1, 0, 5)), ("v", pr.rows_v, (n - 2, 1, d - 1)), ("k", pr.rows_k, (n - 1, 1, 3))):
+        pr.bytes[name][0][p, h, c] = 0x7f
+        rows[0][p, h, c] = float("nan")
+    o, lse = run(pr, pr.cache())
+    out, l64, tol, ltol = paged.attend(pr)
+    o, lse = o.cpu().to(torch.float64), lse.cpu().to(torch.float64)
+    assert torch.isnan(out).any() and torch.equal(torch.isnan(o), torch.isnan(out)) and torch.equal(torch.isnan(lse), torch.isnan(l64))
+    fin = torch.isfinite(out)
+    assert torch.all((o - out).abs()[fin] <= tol[fin])
+
+
+@pytest.mark.parametrize("new", [[1, 3], [90, 2]])
+def test_scales_of_all_sizes(new):
+    """Values from 2^-100 to 2^100, a power of two for each token: the weights of the small ones do not vanish beside their own scale."""
+    pr = paged8.Problem8(4, 128, 16, 8, 2, new, [200, 30])
+    rng = np.random.default_rng(4)
+    for s in range(2):
+        pr.codes["v"][s][:] = rng.integers(1 if s else 100, 247 if s else 200, (pr.kv[s], 1)).astype(np.uint8)
+        pr.rows_v[s] = torch.from_numpy(paged8.of8(pr.bytes["v"][s], pr.codes["v"][s])).to(torch.bfloat16)
+    o, lse = run(pr, pr.cache())
+    out, l64, tol, ltol = paged.attend(pr)
+    assert torch.all((o.cpu().to(torch.float64) - out).abs() <= tol + 2.0 ** -126)      # what is below bf16's normal numbers may vanish
+
+
+@pytest.mark.parametrize("d,P,hq,hkv,new,kv,qb,top", [
+    (128, 64, 32, 8, [1, 1], [640, 70], 1, 4),
+    (128, 16, 28, 4, [37, 0, 5], [300, 3, 5], 16, 9),
+    (64, 32, 8, 2, [70], [300], 64, 7),
+    (128, 64, 8, 2, [130], [600], 128, 6),
+    (256, 128, 4, 2, [20], [700], 8, 4),
+    (64, 16, 8, 2, [1, 1, 1], [90, 200, 7], 64, 5),
+    (128, 16, 4, 1, [300], [400], 200, 9),
+])
+def test_block_attention(d, P, hq, hkv, new, kv, qb, top):
+    pr = paged8.Problem8(13 + d + qb, d, P, hq, hkv, new, kv)
+    rng = np.random.default_rng(d + P)
+    sel = rng.integers(-1, max(-(-n // P) for n in kv) + 1, (pr.tiles(qb), hkv, top)).astype(np.int32)
+    sel[0, 0] = -1
+    sel[-1, -1, 0] = 1 << 30
+    kv_len, table = pr.args()
+    c, dev, want = pr.cache(), torch.from_numpy(sel).cuda(), paged.attend(pr, sel=sel, qb=qb)
+    capped = paged8.attend(pr, 1.0, sel=sel, qb=qb)
+    for bounds in ({}, {"max_new": max(new), "max_kv": max(kv)}):
+        same = dict(q_start=pr.q_start.cuda(), q_block=qb, want_lse=True, **bounds)
+        paged.check(pr, *c.block_attention(pr.q.cuda(), kv_len, table, dev, **same), want)
+        paged.check(pr, *c.block_attention(pr.q.cuda(), kv_len, table, dev, softcap=1.0, **same), capped)
+
+
+# ------------------------------------------------------------------------------------------------ capped scores
+@pytest.mark.parametrize("cap", [0.5, 30.0, 1e6])
+@pytest.mark.parametrize("dtype,d,P,hq,hkv,new,kv,window", [
+    ("bf16", 128, 64, 32, 8, [1, 1, 1], [63, 300, 65], 0),
+    ("bf16", 64, 16, 4, 2, [130], [400], 50),
+    ("bf16", 256, 32, 3, 1, [1, 70], [90, 70], 0),
+    ("fp32", 64, 16, 8, 4, [1, 20], [31, 33], 0),
+    ("fp32", 128, 64, 6, 2, [67], [200], 33),
+    ("fp32", 256, 32, 4, 2, [1, 40], [100, 65], 0),
+    ("e4m3", 128, 16, 28, 4, [5, 0, 33, 1], [5, 0, 40, 17], 0),
+    ("e4m3", 128, 64, 8, 2, [150, 2], [350, 200], 100),
+    ("e4m3", 64, 32, 8, 8, [1, 1], [300, 20], 0),
+    ("e4m3", 256, 64, 4, 2, [150], [150], 0),
+])
+def test_capped_scores(dtype, d, P, hq, hkv, new, kv, window, cap):
+    """Caps far below the scores, about as large and far above: there nothing may be lost to the cap's size."""
+    pr = paged8.problem(dtype, d + P, d, P, hq, hkv, new, kv, scale=4.0)
+    paged.check(pr, *run(pr, pr.cache(), softcap=cap, window=window), paged8.attend(pr, cap, window=window))
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", [1, 3]), ("bf16", [90, 2]), ("fp32", [70, 1]), ("e4m3", [2, 90])])
+def test_capped_rows_that_see_nothing(dtype, new):
+    pr = paged8.problem(dtype, 5, 64, 16, 4, 2, new, [n // 2 for n in new])
+    want = paged8.attend(pr, 20.0)
+    assert torch.isinf(want[1]).any()
+    paged.check(pr, *run(pr, pr.cache(), softcap=20.0), want)
+
+
+def test_capped_blocks():
+    for dtype in ("bf16", "fp32"):
+        pr = paged8.problem(dtype, 6, 128, 16, 8, 2, [40, 1], [200, 90], scale=3.0)
+        sel = np.random.default_rng(6).integers(-1, 13, (pr.tiles(16), 2, 6)).astype(np.int32)
+        kv_len, table = pr.args()
+        o, lse = pr.cache().block_attention(pr.q.cuda(), kv_len, table, torch.from_numpy(sel).cuda(), q_start=pr.q_start.cuda(), q_block=16, softcap=5.0, want_lse=True)
+        paged.check(pr, o, lse, paged8.attend(pr, 5.0, sel=sel, qb=16))
+
+
+# ------------------------------------------------------------------------------------------------ append
+def appended(pr, dtype, k, v, q, rope, inter, q_norm, k_norm, eps, positions, sig, before):
+    """What the cache (arrays of `before` as numpy) and q_out hold after the append, in fp32 steps."""
+    hkv, d, P = pr.hkv, pr.d, pr.P
+    eight = dtype == "e4m3"
+    E = before["k"].shape[-1]
+    rows_type = torch.bfloat16 if eight else paged.DTYPES[dtype]
+    rot = 0 if rope is None else rope.shape[1]
+    out = {n: x.copy() for n, x in before.items()}
+    q_out = np.zeros(q.shape, np.float32)
+    row = 0
+    for s in range(pr.n_seq):
+        n, m = pr.new[s], pr.kv[s]
+        written = {}
+        for i in range(n):
+            p = m - n + i
+            at = p if positions is None else int(positions[row + i])
+            cs = None if rope is None else rope[min(max(at, 0), rope.shape[0] - 1)]
+            qr, kr = q[row + i], k[row + i]
+            if q_norm is not None:
+                qr = paged8.norm(qr, q_norm, eps)
+            if k_norm is not None:
+                kr = paged8.norm(kr, k_norm, eps)
+            q_out[row + i] = paged8.rotate(qr, cs, rot, inter)
+            if p < 0 or not pr.mapped(s, p):
+                continue
+            kr = paged8.rotate(kr, cs, rot, inter)
+            page, slot = int(pr.table[s, p // P]), p % P
+            vr = v[row + i]
+            if eight:
+                kr, ck = paged8.to8(kr)
+                vr, cv = paged8.to8(vr)
+                out["scale"][page, :, 0, slot], out["scale"][page, :, 1, slot] = ck, cv
+            else:
+                kr, vr = (paged8.round_to(x, rows_type).to(torch.float32).numpy() for x in (kr, vr))
+            out["k"][page, :, :, slot] = kr.reshape(hkv, d // E, E)
+            out["v"][page, :, slot // E, :, slot % E] = vr
+            written[page] = slot + 1 if p // P == (m - 1) // P else P
+        if sig:
+            for page, n_slots in written.items():
+                for h in range(hkv):
+                    rows = out["k"][page, h, :, :n_slots].transpose(1, 0, 2).reshape(n_slots, d)
+                    if eight:
+                        rows = paged8.of8(rows, out["scale"][page, h, 0, :n_slots])
+                    out["sig"][page, h] = paged.signature(torch.from_numpy(np.ascontiguousarray(rows)))
+        row += n
+    return out, paged8.round_to(q_out, rows_type)
+
+
+@pytest.mark.parametrize("dtype,d,P,hq,hkv,new,kv,rot,inter,norms,sig,explicit", [
+    ("e4m3", 128, 64, 8, 2, [1, 1, 1], [1, 64, 65], 128, False, "qk", True, False),
+    ("e4m3", 128, 16, 28, 4, [5, 0, 33, 1], [5, 0, 40, 17], 64, True, "", True, False),
+    ("e4m3", 64, 256, 8, 8, [70], [300], 64, False, "k", True, True),
+    ("e4m3", 256, 32, 4, 1, [3, 40], [129, 40], 16, False, "q", False, False),
+    ("e4m3", 128, 64, 4, 2, [200], [201], 0, False, "qk", True, False),
+    ("e4m3", 64, 64, 2, 2, [600], [700], 32, True, "qk", False, False),          # queries of four tokens a workgroup
+    ("bf16", 128, 64, 32, 8, [1, 1], [100, 64], 128, False, "qk", True, False),
+    ("bf16", 64, 16, 7, 7, [19, 40], [19, 77], 48, False, "q", True, True),
+    ("bf16", 256, 128, 4, 2, [150, 0, 2], [300, 5, 2], 256, True, "k", True, False),
+    ("bf16", 128, 32, 2, 1, [520], [530], 0, False, "qk", False, False),
+    ("fp32", 64, 32, 8, 2, [1, 30], [33, 64], 64, False, "qk", True, False),
+    ("fp32", 128, 64, 4, 4, [90], [90], 128, True, "qk", True, False),
+    ("fp32", 256, 16, 3, 1, [20, 1], [20, 16], 32, False, "k", True, False),
+])
+def test_append(dtype, d, P, hq, hkv, new, kv, rot, inter, norms, sig, explicit):
+    """Every byte of the cache: what is written, and what is left as it was.  Queries, keys and values are parts of one projection."""
+    import paper_2601_17702_amd as s3
+    pr = paged8.problem(dtype, 7 + d + P, d, P, hq, hkv, new, kv, **({} if dtype == "e4m3" else {"garbage": 3.0}))
+    rows_type = torch.bfloat16 if dtype == "e4m3" else paged.DTYPES[dtype]
+    g = torch.Generator().manual_seed(d + P)
+    qkv = torch.randn(pr.T, hq + 2 * hkv, d, generator=g) * torch.exp(2 * torch.randn(pr.T, hq + 2 * hkv, 1, generator=g))
+    if pr.T > 4:
+        qkv[1, :, :] = 0.0                                                        # a row of zeros
+        qkv[2, :, 0] = 448.0 * 2.0 ** 5                                           # the largest of a row at the border of its scale, and next to it
+        qkv[3, :, d - 1] = -450.0 * 2.0 ** 9
+    qkv = qkv.to(rows_type)
+    rope = s3.rope_table(max(kv) + 5, rot) if rot else None
+    positions = torch.randint(0, max(kv) + 5, (pr.T,), generator=g, dtype=torch.int32) if explicit else None
+    q_norm = torch.randn(hq, d, generator=g) if "q" in norms else None
+    k_norm = torch.randn(d, generator=g) if "k" in norms else None
+    c = pr.cache(signatures=sig)
+    if sig:
+        c.sig.fill_(7.0)
+
+    def arrays():
+        if dtype == "e4m3":
+            got = {"k": c.k.view(torch.uint8), "v": c.v.view(torch.uint8), "scale": c.codes}
+        else:
+            got = {"k": c.k.float(), "v": c.v.float()}
+        if sig:
+            got["sig"] = c.sig.float()
+        return {n: x.cpu().numpy().copy() for n, x in got.items()}
+    before = arrays()
+    kv_len, table = pr.args()
+    dev = qkv.cuda()
+    q_out = c.append(dev[:, hq:hq + hkv], dev[:, hq + hkv:], kv_len, table, q_start=pr.q_start.cuda(), rope=rope, interleaved=inter, q=dev[:, :hq],
+                     positions=None if positions is None else positions.cuda(), q_norm=None if q_norm is None else q_norm.cuda(),
+                     k_norm=None if k_norm is None else k_norm.cuda(), eps=1e-5)
+    x = qkv.to(torch.float32).numpy()
+    want, want_q = appended(pr, dtype, x[:, hq:hq + hkv], x[:, hq + hkv:], x[:, :hq], None if rope is None else rope.cpu().numpy(), inter,
+                            None if q_norm is None else q_norm.numpy(), None if k_norm is None else k_norm.numpy(), 1e-5, positions, sig, before)
+    assert torch.equal(q_out.cpu(), want_q)
+    for name, got in arrays().items():
+        np.testing.assert_array_equal(got, want[name], err_msg=name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32", "e4m3"])
+def test_append_of_what_is_not_finite(dtype):
+    """Infinities and NaN in a row: normed by what the formula gives, in 8 bits NaN and no part of the scale; other rows are as they would be without."""
+    import paper_2601_17702_amd as s3
+    pr = paged8.problem(dtype, 8, 64, 16, 4, 2, [6], [6], **({} if dtype == "e4m3" else {"garbage": 0.0}))
+    x = torch.randn(6, 8, 64, generator=torch.Generator().manual_seed(8))
+    x[0, :, 3] = float("inf")
+    x[1, :, 5] = float("nan")
+    x[2, :, 7] = -float("inf")
+    x[3, :, 9] = 3e38
+    x[4] *= 1e-38
+    x = x.to(torch.bfloat16 if dtype == "e4m3" else paged.DTYPES[dtype])
+    for norms in (False, True):
+        c = pr.cache()
+        kv_len, table = pr.args()
+        w = torch.ones(64, device="cuda") if norms else None
+        d = x.cuda()
+        q_out = c.append(d[:, 4:6], d[:, 6:], kv_len, table, q_start=pr.q_start.cuda(), q=d[:, :4], q_norm=w, k_norm=w, eps=1e-20)
+        k, v = c.read(kv_len, table, 6, q_start=pr.q_start.cuda())
+        f = x.to(torch.float32).numpy()
+        one = np.ones(64, np.float32)
+        for got, src in ((q_out, f[:, :4]), (k, f[:, 4:6]), (v, f[:, 6:])):
+            want = src
+            if norms and src is not f[:, 6:] and got is not v:
+                want = paged8.norm(src, one, 1e-20)
+            if dtype == "e4m3" and got is not q_out:
+                want = paged8.of8(*paged8.to8(want))
+            want = torch.from_numpy(np.ascontiguousarray(want)).to(got.dtype)
+            assert torch.equal(torch.isnan(got.cpu()), torch.isnan(want))
+            assert torch.equal(torch.nan_to_num(got.cpu(), nan=1.0), torch.nan_to_num(want, nan=1.0))
+
+
+@pytest.mark.parametrize("dtype", ["e4m3", "bf16"])
+def test_append_token_by_token_equals_one_chunk(dtype):
+    import paper_2601_17702_amd as s3
+    n, P, hkv, d = 150, 32, 2, 128
+    x = torch.randn(n, 2 * hkv, d, device="cuda").to(torch.bfloat16)
+    table = torch.randperm(6, device="cuda").to(torch.int32)[None]
+    rope, w = s3.rope_table(n, d), torch.rand(d, device="cuda") + 0.5
+    caches = []
+    for step in (n, 1):
+        c = s3.KVCache8(6, P, hkv, d, signatures=True) if dtype == "e4m3" else s3.KVCache(6, P, hkv, d, signatures=True)
+        for t in (c.k, c.v, c.sig, *([c.codes] if dtype == "e4m3" else [])):
+            t.view(torch.uint8).zero_()
+        for i in range(0, n, step):
+            c.append(x[i:i + step, :hkv], x[i:i + step, hkv:], torch.tensor([i + step], dtype=torch.int32, device="cuda"), table,
+                     q_start=torch.tensor([0, step], dtype=torch.int32, device="cuda"), rope=rope, k_norm=w)
+        caches.append(c)
+    a, b = caches
+    for name in ("k", "v", "sig") + (("codes",) if dtype == "e4m3" else ()):
+        assert torch.equal(getattr(a, name).view(torch.uint8), getattr(b, name).view(torch.uint8)), name
+
+
+# ------------------------------------------------------------------------------------------------ read
+@pytest.mark.parametrize("dtype,d,P,hkv,new,kv", [
+    ("e4m3", 128, 64, 8, [1, 1, 1], [63, 64, 65]), ("e4m3", 64, 16, 2, [130, 0, 5], [130, 3, 400]), ("e4m3", 256, 256, 1, [300], [700]),
+    ("bf16", 128, 64, 2, [70, 1], [90, 1]), ("bf16", 256, 16, 1, [200], [200]), ("bf16", 64, 128, 3, [65], [500]),
+    ("fp32", 64, 32, 2, [100], [133]), ("fp32", 128, 16, 1, [7, 65], [9, 65]), ("fp32", 256, 64, 2, [90], [90]),
+])
+def test_read(dtype, d, P, hkv, new, kv):
+    pr = paged8.problem(dtype, 9 + d, d, P, hkv, hkv, new, kv)
+    pr.table[-1, 0] = -1                                                          # zeros come of a page that is not there
+    c = pr.cache()
+    kv_len, table = pr.args()
+    qs = pr.q_start.cuda()
+
+    def want(positions):
+        k, v = (torch.zeros(pr.T, hkv, d, dtype=pr.dtype) for _ in "kv")
+        row = 0
+        for s in range(pr.n_seq):
+            for i in range(new[s]):
+                p = int(positions[row + i])
+                if 0 <= p < kv[s] and pr.mapped(s, p):
+                    k[row + i], v[row + i] = pr.rows_k[s][p], pr.rows_v[s][p]
+            row += new[s]
+        return k, v
+    last = torch.cat([torch.arange(m - n, m) for n, m in zip(new, kv)])
+    g = torch.Generator().manual_seed(d)
+    anywhere = torch.cat([torch.randint(-2, m + 40, (n,), generator=g) for n, m in zip(new, kv)])
+    spans = torch.cat([(torch.arange(n) // 5 * 23 + torch.arange(n) % 5) % max(m, 1) for n, m in zip(new, kv)])
+    for positions in (None, anywhere, anywhere.sort(descending=True).values, spans, torch.full((pr.T,), 1 << 30), torch.full((pr.T,), -(1 << 31))):
+        dev = None if positions is None else positions.to(torch.int32).cuda()
+        got = c.read(kv_len, table, pr.T, q_start=qs, positions=dev)
+        for a, b in zip(got, want(last if positions is None else positions)):
+            assert torch.equal(a.cpu(), b)
+    if max(new) == 1:
+        a = c.read(kv_len, table, pr.T)
+        assert all(torch.equal(x.cpu(), y) for x, y in zip(a, want(last)))
+
+
+def test_read_leaves_rows_of_no_sequence():
+    pr = paged8.Problem8(10, 64, 16, 2, 2, [3, 4], [30, 40])
+    kv_len, table = pr.args()
+    qs = torch.tensor([2, 5, 9], dtype=torch.int32, device="cuda")
+    k, v = (torch.full((12, 2, 64), 5.0, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    pr.cache().read(kv_len, table, 12, q_start=qs, k_out=k, v_out=v)
+    for x, rows in ((k, pr.rows_k), (v, pr.rows_v)):
+        assert torch.equal(x[2:9].cpu(), torch.cat([rows[0][27:30], rows[1][36:40]]))
+        assert torch.all(x[:2] == 5.0) and torch.all(x[9:] == 5.0)
+
+
+# ------------------------------------------------------------------------------------------------ of all of them
+@pytest.mark.parametrize("new", [1, 40, 100])
+def test_offsets_past_32_bits(new):
+    """A cache of 4.9 GB of keys and as much of values, the sequence in its last pages."""
+    import paper_2601_17702_amd as s3
+    P, hkv, d, kv = 64, 8, 128, 200
+    pr = paged8.Problem8(11, d, P, 32, hkv, [new], [kv])
+    small = pr.cache()
+    n_pages = 75000
+    c = s3.KVCache8(n_pages, P, hkv, d)
+    far = pr.table.clone()
+    used = far[0, :4].long()
+    far[0, :4] += n_pages - pr.n_pages
+    for a, b in ((c.k, small.k), (c.v, small.v), (c.codes, small.codes)):
+        a.view(torch.uint8)[used.cuda() + (n_pages - pr.n_pages)] = b.view(torch.uint8)[used.cuda()]
+    kv_len, table = pr.args()
+    q, qs = pr.q.cuda(), pr.q_start.cuda()
+    o, lse = c.attention(q, kv_len, far.cuda(), q_start=qs, want_lse=True)
+    paged.check(pr, o, lse, paged.attend(pr))
+    k, v = c.read(kv_len, far.cuda(), new, q_start=qs)
+    assert torch.equal(k.cpu(), pr.rows_k[0][kv - new:]) and torch.equal(v.cpu(), pr.rows_v[0][kv - new:])
+    x = torch.randn(new, 2 * hkv, d, device="cuda").to(torch.bfloat16)
+    for cache, t in ((small, table), (c, far.cuda())):
+        cache.append(x[:, :hkv], x[:, hkv:], kv_len, t, q_start=qs)
+    for a, b in ((c.k, small.k), (c.v, small.v), (c.codes, small.codes)):
+        assert torch.equal(a.view(torch.uint8)[used.cuda() + (n_pages - pr.n_pages)], b.view(torch.uint8)[used.cuda()])
+
+
+@pytest.mark.parametrize("starts", [[0, 5, 60, 60], [0, 30, 10, 40], [0, 40, 90, 100], [2, -3, 8, 40]])
+def test_starts_that_are_no_starts_write_nothing_else(starts):
+    """Whatever the starts hold, nothing outside the call's arrays is read or written: rows beside them keep their values."""
+    pr = paged8.Problem8(12, 64, 16, 4, 2, [20, 20, 20], [40, 50, 60])
+    c = pr.cache(signatures=True)
+    c.sig.zero_()
+    kv_len, table = pr.args()
+    qs = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    room = torch.full((70, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(64, device="cuda")
+    x = torch.randn(60, 8, 64, device="cuda").to(torch.bfloat16)
+    c.append(x[:, :2], x[:, 2:4], kv_len, table, q_start=qs, q=x[:, 4:], q_out=room[:60], q_norm=w, k_norm=w)
+    assert torch.all(room[60:] == 3.0)
+    c.attention(x[:, 4:], kv_len, table, q_start=qs, out=room[:60])
+    c.attention(x[:, 4:], kv_len, table, q_start=qs, out=room[:60], softcap=9.0)
+    rk, rv = (torch.full((70, 2, 64), 3.0, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    c.read(kv_len, table, 60, q_start=qs, k_out=rk[:60], v_out=rv[:60])
+    torch.cuda.synchronize()
+    assert torch.all(room[60:] == 3.0) and torch.all(rk[60:] == 3.0) and torch.all(rv[60:] == 3.0)
+
+
+def test_choice_of_blocks_reads_signatures_only():
+    pr = paged8.Problem8(13, 128, 16, 8, 2, [1, 30], [300, 200])
+    sig = torch.randint(-128, 129, (pr.n_pages, 2, 128), generator=pr.g).to(torch.float32).mul(2.0 ** -6).to(torch.bfloat16)
+    kv_len, table = pr.args()
+    sel = pr.cache(sig=sig).select(pr.q.cuda(), kv_len, table, 7, q_start=pr.q_start.cuda(), q_block=8)
+    assert np.array_equal(sel.cpu().numpy(), paged.select(pr, sig, 7, 8, 1, 1))
+
+
+@pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("new", [[1, 1, 1], [40, 1, 100]])
+def test_used_together_and_captured_in_a_graph(new, eight):
+    """Norms, append, attention with and without a cap, choice, listed blocks and read-back, recorded once: every replay, with other inputs in the same
+    places and eager work between, equals the eager calls, on a stream of its own too."""
+    import paper_2601_17702_amd as s3
+    pr = paged8.problem("e4m3" if eight else "bf16", 14, 128, 64, 8, 2, new, [200, 300, 1000])
+    c = pr.cache(signatures=True)
+    c.sig.zero_()
+    kv_len, table = pr.args()
+    qs = pr.q_start.cuda()
+    rope = s3.rope_table(1000, 128)
+    w = torch.rand(128, device="cuda") + 0.5
+    qkv = torch.randn(pr.T, 12, 128, device="cuda").to(torch.bfloat16)
+
+    def step():
+        q = c.append(qkv[:, 8:10], qkv[:, 10:], kv_len, table, q_start=qs, rope=rope, q=qkv[:, :8], q_norm=w, k_norm=w)
+        o, _ = c.attention(q, kv_len, table, q_start=qs, max_new=max(new), max_kv=1000)
+        oc, _ = c.attention(q, kv_len, table, q_start=qs, max_new=max(new), max_kv=1000, softcap=10.0)
+        sel = c.select(q, kv_len, table, 6, q_start=qs, q_block=16, max_kv=1000)
+        ob, _ = c.block_attention(q, kv_len, table, sel, q_start=qs, q_block=16, max_new=max(new), softcap=10.0)
+        return q, o, oc, sel, ob, *c.read(kv_len, table, pr.T, q_start=qs)
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        there = [t.clone() for t in step()]
+    torch.cuda.current_stream().wait_stream(st)
+    torch.cuda.synchronize()
+    for a, b in zip(there, step()):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(4):
+        qkv.copy_(torch.randn(pr.T, 12, 128, device="cuda"))
+        graph.replay()
+        got = [t.clone() for t in out]
+        torch.cuda.synchronize()
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b)
+
+
+def test_no_tokens_is_a_no_op():
+    pr = paged8.Problem8(17, 128, 64, 8, 2, [0, 0], [10, 0])
+    kv_len, table = pr.args()
+    c = pr.cache(signatures=True)
+    qs = pr.q_start.cuda()
+    x = torch.zeros(0, 2, 128, dtype=torch.bfloat16, device="cuda")
+    c.append(x, x, kv_len, table, q_start=qs, k_norm=torch.ones(128, device="cuda"))
+    assert c.attention(pr.q.cuda(), kv_len, table, q_start=qs)[0].shape == (0, 8, 128)
+    k, v = c.read(kv_len, table, 0, q_start=qs)
+    assert k.shape == v.shape == (0, 2, 128)
+
+
+def test_refusals():
+    import paper_2601_17702_amd as s3
+    pr = paged8.Problem8(16, 128, 64, 8, 2, [1], [10])
+    c = pr.cache()
+    kv_len, table = pr.args()
+    q = pr.q.cuda()
+    w = torch.ones(128, device="cuda")
+    for call in (
+        lambda: s3.KVCache8(4, 48, 2, 128).attention(q, kv_len, table),
+        lambda: c.attention(q[:, :7], kv_len, table),
+        lambda: c.attention(q, kv_len, table, softcap=-1.0),
+        lambda: c.attention(q, kv_len, table, softcap=float("nan")),
+        lambda: c.attention(q, kv_len, table, softcap=float("inf")),
+        lambda: c.attention(q, kv_len, table, scale=1e25, softcap=1e-25),
+        lambda: c.attention(q, kv_len, table, window=-1),
+        lambda: c.select(q, kv_len, table, 4),
+        lambda: c.append(q[:, :2], q[:, 2:4], kv_len, table, k_norm=w, eps=0.0),
+        lambda: c.append(q[:, :2], q[:, 2:4], kv_len, table, k_norm=torch.ones(132, device="cuda")[1:129]),
+        lambda: c.read(kv_len, table, 1, k_out=torch.zeros(264, dtype=torch.bfloat16, device="cuda")[1:257].view(1, 2, 128)),
+    ):
+        with pytest.raises(s3.S3Error) as e:
+            call()
+        assert e.value.code == -1
+    for call in (
+        lambda: c.attention(q.float(), kv_len, table),
+        lambda: c.append(q[:, :2], q[:, 2:4], kv_len, table, q_norm=w),                       # no queries to norm
+        lambda: c.append(q[:, :2], q[:, 2:4], kv_len, table, k_norm=w[:64]),
+        lambda: c.append(q[:, :2], q[:, 2:4], kv_len, table, k_norm=w.to(torch.bfloat16)),
+        lambda: c.read(kv_len, table, 1, positions=torch.zeros(2, dtype=torch.int32, device="cuda")),
+        lambda: s3.KVCache8(4, 64, 2, 128, k=torch.zeros(4, 2, 8, 64, 16, dtype=torch.uint8, device="cuda")),
+    ):
+        with pytest.raises(AssertionError):
+            call()
