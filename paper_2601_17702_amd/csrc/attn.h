@@ -38,8 +38,8 @@ struct AttnArgs {
     int64_t q_ts, q_hs;       // bytes
     int n_kv, G, n_q, window;
     int qb, top, per_q, lists;// lists: tokens a tile, entries, row tiles a tile of queries (tiled kernel), how many lists there are
-    float sl;                 // scale * log2(e); 1 with a cap, whose scores come scaled
-    float cap, to_cap;        // cap * log2(e), or 0: none; scale / cap
+    float sl;                 // scale * log2(e), or what capped scores are to be multiplied by
+    float cap, to_cap, cap_lse;      // with a cap (0: none): cap * log2(e), scale / cap, and what lse is less by where the capped scores come shifted
     int few;                  // sequences of at most this many rows are the streaming kernel's
 };
 
@@ -214,16 +214,16 @@ struct AttnState {
         asm volatile("" : "+v"(l));      // summed here, not behind the products: nothing else would run beside it there
         return w;
     }
-    // The same of an 8-bit cache's 8 tokens, times what their values are to be scaled by (codes: a byte each): a power of two, so that nothing
+    // The same of an 8-bit cache's 8 tokens, times what their values are to be scaled by (f: of four tokens each): a power of two, so that nothing
     // more is rounded, and one multiplication a weight in place of one for each of a token's values.
-    __device__ __forceinline__ vec weights(const kv_f32x16& s, int y, float sl, float sub, unsigned codes0, unsigned codes1) {
+    __device__ __forceinline__ vec weights(const kv_f32x16& s, int y, float sl, float sub, kv_f32x4 f0, kv_f32x4 f1) {
         vec w;
         float part = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float x = __builtin_amdgcn_exp2f(s[y * E + e] * sl - sub);
             part = e ? part + x : x;
-            w[e] = (T)(x * kv_scale((e < 4 ? codes0 : codes1) >> (e % 4 * 8)));
+            w[e] = (T)(x * (e < 4 ? f0[e % 4] : f1[e % 4]));
         }
         l += part;
         asm volatile("" : "+v"(l));
@@ -245,11 +245,27 @@ struct AttnState {
     }
 };
 
-// Capped scores: c tanh(z) for this lane's raw scores x, z = x u, c in log2 units.  Below |z| = 0.35 by tanh's series (its next term, 1382 z^11 / 155925, is
-// 2^-22 of z there), above as 1 - 2 / (1 + exp(2 z)), whose error of 2^-23 or so is relative to one.  Where all of a wavefront's are small, as a cap well above
-// the scores leaves them, only the series runs: 7 instructions a score; the exponential, the reciprocal and the choice are 44 cycles more.
+// Capped scores of this lane's raw ones x: c tanh(z), z = x u, in log2 units.
+//
+// NEAR: c tanh(z) = 2 c r - c with r = 1 / (1 + exp(-2 z)); r takes the score's place, 2 c that of the scale, and softmax does not see the shift, which lse takes off
+// at the end: a multiplication, an addition and two quarter-rate instructions a score more than without a cap.  r is off by 2^-23 or so, the score by 2^-22 c: for
+// rows of bf16, whose weights are rounded to 2^-8 of themselves, up to caps of 2048 (5e-4 there).
+// Otherwise, for scores as exact as fp32 ones whatever the cap: below |z| = 0.35 by tanh's series (its next term, 1382 z^11 / 155925, is 2^-22 of z there), above as
+// 1 - 2 / (1 + exp(2 z)).  Where all of a wavefront's are small, as a cap well above the scores leaves them, only the series runs.
+// us with the second / with the first, chunks of 333, 826 and 2048 tokens that see 4096 each, 32 heads over 8, bf16: 484 / 342.
+constexpr float kS3NearCap = 2048.0f;
 template <int N>
-__device__ __forceinline__ void kv_cap(kv_f32x16 (&s)[N], float u, float c) {
+__device__ __forceinline__ void kv_cap_near(kv_f32x16 (&s)[N], const AttnArgs& p) {
+    const float k = -2.8853900817779268f * p.to_cap;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[x][i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[x][i] * k));
+}
+__device__ __forceinline__ bool kv_near(const AttnArgs& p) { return p.cap_lse != 0.0f; }
+template <int N>
+__device__ __forceinline__ void kv_cap_far(kv_f32x16 (&s)[N], const AttnArgs& p) {
+    const float u = p.to_cap, c = p.cap;
     float most = 0.0f;
 #pragma unroll
     for (int x = 0; x < N; ++x)
@@ -270,6 +286,12 @@ __device__ __forceinline__ void kv_cap(kv_f32x16 (&s)[N], float u, float c) {
                 s[x][i] = small;
             }
         }
+}
+
+template <bool BF16, int N>
+__device__ __forceinline__ void kv_cap(kv_f32x16 (&s)[N], const AttnArgs& p) {
+    if (BF16 && kv_near(p)) kv_cap_near(s, p);
+    else kv_cap_far(s, p);
 }
 
 // 1 / l, or what makes a row that saw nothing 0 (infinity makes NaN of one that saw only scores of -inf); its lse.

@@ -40,6 +40,7 @@ constexpr int kS3E4m3 = 2;             // s3_kv_cache.dtype inside the library; 
 
 // Code c of a scale: 2^(c - 127), for c from 1 to 247, all that an append writes; others count as the nearer of the two.
 __device__ __forceinline__ float kv_scale(unsigned code) { return __builtin_amdgcn_fmed3f(__uint_as_float((code & 255u) << 23), 0x1p-126f, 0x1p120f); }
+__device__ __forceinline__ kv_f32x4 kv_scales(unsigned codes) { return kv_f32x4{kv_scale(codes), kv_scale(codes >> 8), kv_scale(codes >> 16), kv_scale(codes >> 24)}; }
 // The smallest code >= 1 that leaves nothing above 448, the largest e4m3 value: max_abs_bits are a finite float's.
 __device__ __forceinline__ unsigned kv_scale_code(unsigned max_abs_bits) {
     return (unsigned)max((int)(max_abs_bits >> 23) - 8 + ((max_abs_bits & 0x7fffffu) > 0x600000u ? 1 : 0), 1);

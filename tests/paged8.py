@@ -95,7 +95,9 @@ def problem(dtype, seed, d, P, hq, hkv, new, kv, garbage=float("nan"), **more):
 
 def attend(pr, cap, window=0, scale=None, sel=None, qb=None):
     """As paged.attend, with scores cap * tanh(score / cap).  The score's own error shrinks with tanh's slope, at most 1; tanh is good to 2^-20 of the
-    capped score, which the bounds take for its largest."""
+    capped score, which the bounds take for its largest.  Over rows of bf16 and with caps up to 2048 a score comes as 2 cap r - cap, r = 1 / (1 + exp(-2 z)) in
+    (0, 1): r is off by half a unit of its reciprocal (2^-24) and by r (1 - r) <= 1/4 of its exponential's relative error (2^-22 with its argument's rounding, 2^-24
+    |2 z| log2(e) r (1 - r) being less), so by less than 2^-23, and the score by 2^-22 of the cap."""
     scale = pr.d ** -0.5 if scale is None else scale
     G, T = pr.hq // pr.hkv, pr.T
     out = torch.zeros(T, pr.hq, pr.d, dtype=F64)
@@ -129,6 +131,8 @@ def attend(pr, cap, window=0, scale=None, sel=None, qb=None):
                 out[row + i, h * G:(h + 1) * G] = o
                 lse[row + i, h * G:(h + 1) * G] = torch.logsumexp(z, 1)
                 e = (pr.d * 2.0 ** -24 * scale * (q.abs() @ k.abs().t()) + 2.0 ** -20 * z.abs() + 2.0 ** -23 * z.abs()).amax(1) + 2.0 ** -21
+                if bf and cap <= 2048:
+                    e = e + 2.0 ** -22 * cap
                 rel = 2 * e + len(idx) * 2.0 ** -24 + (2.0 ** -8 if bf else 0.0)
                 tol[row + i, h * G:(h + 1) * G] = rel[:, None] * (p @ v.abs()) + (2.0 ** -8 if bf else 2.0 ** -24) * o.abs() * 1.01
                 ltol[row + i, h * G:(h + 1) * G] = e + len(idx) * 2.0 ** -24 + 2.0 ** -22 * lse[row + i, h * G:(h + 1) * G].abs()

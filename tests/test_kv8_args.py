@@ -97,7 +97,7 @@ def test_nothing_to_do():
 def test_sizes():
     assert s3._KV8_CACHE.size == 48 and s3._KV_NORM.size == 40 and C.sizeof(C.c_void_p) == 8
     L = s3.lib()
-    for b, n_q in ((batch(), 8), (batch(n_tokens=600, max_new=500), 32), (batch(qs=0, n_tokens=2, max_new=1), 8)):
+    for b, n_q in ((batch(), 8), (batch(n_tokens=600, max_new=600), 32), (batch(qs=0, n_tokens=2, max_new=1), 8)):
         assert L.s3_kv8_attention_workspace(cache(), b, n_q) == L.s3_paged_attention_workspace(cache16(), b, n_q) > 0
 
 
