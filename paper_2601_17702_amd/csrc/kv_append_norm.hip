@@ -5,13 +5,14 @@
 //   code c = the smallest that leaves max|x| 2^(127 - c) <= 448, element = e4m3(x 2^(127 - c)), to nearest even
 // A power of two as a scale costs no precision (e4m3 values have the same 4 bits in every octave of 17) and makes both scalings exact.
 //
-// What bounds it: memory.  A row of d channels lies in d / 8 lanes, 8 channels each: where pairs are (i, i + rot / 2) four of one half and
-// their four partners, so a rotation needs no other lane's channels and a norm's sum only log2(d / 8) exchanges.
+// What bounds it: memory.  A row of d channels lies in d / 16 lanes, 16 channels each: where pairs are (i, i + rot / 2) eight of one half and
+// their eight partners, so a rotation needs no other lane's channels, and a norm's sum is exchanged between neighbours of a row of 16 lanes only.
 #include "kv_cache.h"
 
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kDeep = 2;               // rows of a thread whose loads are under way at a time
 constexpr int kSlots = 64;             // slots of a page that pass through LDS at a time
 
 struct NormArgs {
@@ -34,47 +35,61 @@ struct NormArgs {
     int group;                                       // tokens of such a one
 };
 
-template <typename T> struct Four {
-    typedef __attribute__((ext_vector_type(4))) T vec;
-};
+constexpr int kChannels = 16;          // of a row in one lane
 
-// This lane's 8 channels of a row: c0 .. c0 + 3 and c1 .. c1 + 3.
+// This lane's channels of a row: c0 .. c0 + 7 and c1 .. c1 + 7.  Two halves of the row's, so that neighbouring lanes have neighbouring pieces, but where
+// the rotation's halves are shorter than those.
 template <int D>
 struct Place {
     int lane, c0, c1;
-    bool turned;                                     // they are pairs of the rotation
+    bool turn0, turn1;                               // they are in the rotation
     __device__ __forceinline__ Place(const NormArgs& p) {
-        lane = threadIdx.x & (D / 8 - 1);
-        turned = p.rope && lane * 8 < p.rot;
-        const bool apart = turned && !p.inter;
-        c0 = apart ? lane * 4 : lane * 8;
-        c1 = apart ? p.rot / 2 + lane * 4 : lane * 8 + 4;
+        lane = threadIdx.x & (D / kChannels - 1);
+        const bool apart = p.rope && !p.inter, in = apart && lane * 16 < p.rot;
+        c0 = apart && !in ? lane * 16 : lane * 8;
+        c1 = in ? p.rot / 2 + lane * 8 : apart ? lane * 16 + 8 : D / 2 + lane * 8;
+        turn0 = in || (p.rope && p.inter && c0 < p.rot);
+        turn1 = in || (p.rope && p.inter && c1 < p.rot);
     }
 };
 
+// Those of a row as they are loaded, and as numbers.
 template <typename T>
-__device__ __forceinline__ void load_row(const char* row, int c0, int c1, float (&x)[8]) {
-    typedef typename Four<T>::vec vec;
-    const vec a = *(const vec*)(row + c0 * (int)sizeof(T)), b = *(const vec*)(row + c1 * (int)sizeof(T));
+struct Raw {
+    typedef typename KvElem<T>::vec vec;
+    static constexpr int E = KvElem<T>::E, N = 8 / E;
+    vec a[2 * N];
+    __device__ __forceinline__ void load(const char* row, int c0, int c1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[i] = (float)a[i];
-        x[4 + i] = (float)b[i];
+        for (int y = 0; y < 2 * N; ++y) a[y] = *(const vec*)(row + ((y < N ? c0 : c1) + y % N * E) * (int)sizeof(T));
+    }
+    __device__ __forceinline__ void get(float (&x)[16]) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = (float)a[i / E][i % E];
+    }
+};
+
+// x of the lane that a step of a reduction over 2, 4, 8 or 16 neighbours adds: the other of a pair, of a four's halves, the mirrored one of eight and of sixteen.
+template <int STEP>
+__device__ __forceinline__ unsigned neighbour(unsigned x) {
+    constexpr int ctrl = STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : STEP == 4 ? 0x141 : 0x140;
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, 0xf, 0xf, true);
+}
+// Sum, and largest, over the LANES lanes of a row, in every one of them.
+template <int LANES, int STEP = 1>
+__device__ __forceinline__ double row_sum(double x) {
+    if constexpr (STEP < LANES) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, x);
+        const uint64_t o = (uint64_t)neighbour<STEP>((unsigned)(u >> 32)) << 32 | neighbour<STEP>((unsigned)u);
+        return row_sum<LANES, STEP * 2>(x + __builtin_bit_cast(double, o));
+    } else {
+        return x;
     }
 }
-
-// Sum over the D / 8 lanes of a row, in every one of them.
-template <int D>
-__device__ __forceinline__ double row_sum(double x) {
-#pragma unroll
-    for (int m = 1; m < D / 8; m *= 2) x += __shfl_xor(x, m);
-    return x;
-}
-template <int D>
+template <int LANES, int STEP = 1>
 __device__ __forceinline__ unsigned row_max(unsigned x) {
-#pragma unroll
-    for (int m = 1; m < D / 8; m *= 2) x = max(x, (unsigned)__shfl_xor((int)x, m));
-    return x;
+    if constexpr (STEP < LANES) return row_max<LANES, STEP * 2>(max(x, neighbour<STEP>(x)));
+    else return x;
 }
 
 // 1 / sqrt(t) to the last bit or so of 64: the unit's estimate is good to 2^-24, each step squares its error.
@@ -88,59 +103,83 @@ __device__ __forceinline__ double inverse_root(double t) {
 
 // Norm (w: the head's weights, or null) and rotation (turn: the position's cosines and sines) of this lane's channels.
 template <int D>
-__device__ __forceinline__ void norm_turn(const NormArgs& p, const Place<D>& at, const float* w, const float* turn, float (&x)[8]) {
+__device__ __forceinline__ void norm_turn(const NormArgs& p, const Place<D>& at, const float* w, const float* turn, float (&x)[16]) {
 #pragma clang fp contract(off)
-    kv_f32x4 c, s;
-    if (at.turned) {
-        c = *(const kv_f32x4*)(turn + at.lane * 4);
-        s = *(const kv_f32x4*)(turn + p.rot / 2 + at.lane * 4);
-    }
+    kv_f32x4 c[2], s[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+        if (y ? at.turn1 : at.turn0) {
+            const float* from = turn + (p.inter ? (y ? at.c1 : at.c0) / 2 : at.lane * 8 + y * 4);
+            c[y] = *(const kv_f32x4*)from;
+            s[y] = *(const kv_f32x4*)(from + p.rot / 2);
+        }
     if (w) {
-        const kv_f32x4 w0 = *(const kv_f32x4*)(w + at.c0), w1 = *(const kv_f32x4*)(w + at.c1);
         double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fma((double)x[i], (double)x[i], sum);
-        const float r = (float)inverse_root(row_sum<D>(sum) * (1.0 / D) + p.eps);
+        for (int i = 0; i < 16; ++i) sum = fma((double)x[i], (double)x[i], sum);
+        const float r = (float)inverse_root(row_sum<D / kChannels>(sum) * (1.0 / D) + p.eps);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = x[i] * r * w0[i];
-            x[4 + i] = x[4 + i] * r * w1[i];
+        for (int y = 0; y < 4; ++y) {
+            const kv_f32x4 f = *(const kv_f32x4*)(w + (y < 2 ? at.c0 : at.c1) + y % 2 * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[y * 4 + i] = x[y * 4 + i] * r * f[i];
         }
     }
-    if (at.turned) {
+    if (p.inter) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int a = p.inter ? 2 * i : i, b = p.inter ? 2 * i + 1 : 4 + i;
-            const float u = x[a], v = x[b];
-            x[a] = u * c[i] - v * s[i];
-            x[b] = v * c[i] + u * s[i];
+        for (int y = 0; y < 2; ++y)
+            if (y ? at.turn1 : at.turn0)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float u = x[y * 8 + 2 * i], v = x[y * 8 + 2 * i + 1];
+                    x[y * 8 + 2 * i] = u * c[y][i] - v * s[y][i];
+                    x[y * 8 + 2 * i + 1] = v * c[y][i] + u * s[y][i];
+                }
+    } else if (at.turn0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float u = x[i], v = x[8 + i];
+            x[i] = u * c[i / 4][i % 4] - v * s[i / 4][i % 4];
+            x[8 + i] = v * c[i / 4][i % 4] + u * s[i / 4][i % 4];
         }
     }
 }
 
 // This lane's channels in 8 bits, and the row's code.  What is not finite becomes NaN, and counts for nothing in the scale.
 template <int D>
-__device__ __forceinline__ void to8(const float (&x)[8], unsigned& lo, unsigned& hi, unsigned& code) {
+__device__ __forceinline__ kv_u32x4 to8(const float (&x)[16], unsigned& code) {
     unsigned most = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 16; ++i) {
         const unsigned a = __float_as_uint(x[i]) & 0x7fffffffu;
         most = max(most, a < 0x7f800000u ? a : 0u);
     }
-    code = kv_scale_code(row_max<D>(most));
+    code = kv_scale_code(row_max<D / kChannels>(most));
     const float by = __uint_as_float((254u - code) << 23);
-    float y[8];
+    kv_u32x4 u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = fabsf(x[i]) < INFINITY ? x[i] * by : __uint_as_float(0x7fc00000u);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false), true);
+    for (int k = 0; k < 4; ++k) {
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = fabsf(x[4 * k + i]) < INFINITY ? x[4 * k + i] * by : __uint_as_float(0x7fc00000u);
+        u[k] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
+    }
+    return u;
 }
 
 template <typename T>
-__device__ __forceinline__ void store_row(char* row, int c0, int c1, const float (&x)[8]) {
-    typedef typename Four<T>::vec vec;
-    *(vec*)(row + c0 * (int)sizeof(T)) = vec{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
-    *(vec*)(row + c1 * (int)sizeof(T)) = vec{(T)x[4], (T)x[5], (T)x[6], (T)x[7]};
+__device__ __forceinline__ void store_row(char* row, int c0, int c1, const float (&x)[16]) {
+    typedef typename KvElem<T>::vec vec;
+    constexpr int E = KvElem<T>::E;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int y = 0; y < 8 / E; ++y) {
+            vec a;
+#pragma unroll
+            for (int i = 0; i < E; ++i) a[i] = (T)x[h * 8 + y * E + i];
+            *(vec*)(row + ((h ? c1 : c0) + y * E) * (int)sizeof(T)) = a;
+        }
 }
 
 __device__ __forceinline__ const float* turn_of(const NormArgs& p, int token, int pos) {
@@ -152,7 +191,7 @@ __device__ __forceinline__ const float* turn_of(const NormArgs& p, int token, in
 template <typename S, int D>
 __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(NormArgs p) {
     typedef typename KvStore<S>::row T;
-    constexpr int E = KvStore<S>::E, ES = KvStore<S>::BYTES, NG = D / E, L = D / 8, SIDE = kThreads / L, ROW = D * ES + 16;
+    constexpr int E = KvStore<S>::E, ES = KvStore<S>::BYTES, NG = D / E, L = D / kChannels, SIDE = kThreads / L, ROW = D * ES + 16;
     constexpr bool EIGHT = KvStore<S>::EIGHT;
     constexpr int SLAB = D * ES >= 1024 ? 16 : D * ES >= 512 ? 32 : kSlots;
     const int tid = threadIdx.x;
@@ -183,14 +222,24 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(NormArgs p) {
         }
         __syncthreads();
         const int rows = (t1 - t0) * p.n_q;
-#pragma unroll 2
-        for (int r = tid / L; r < rows; r += SIDE) {
-            const int t = r / p.n_q, head = r - t * p.n_q, token = t0 + t, pos = place[t];
-            if (pos == 1 << 30) continue;            // the same for all lanes of a row
-            float x[8];
-            load_row<T>(p.q + token * p.q_ts + head * p.q_hs, at.c0, at.c1, x);
-            norm_turn<D>(p, at, p.q_norm ? p.q_norm + head * p.q_nhs : nullptr, at.turned ? turn_of(p, token, pos) : nullptr, x);
-            store_row<T>(p.q_out + ((int64_t)token * p.n_q + head) * (D * (int)sizeof(T)), at.c0, at.c1, x);
+        for (int r0 = tid / L; r0 < rows; r0 += SIDE * kDeep) {      // kDeep rows' loads before the first store
+            Raw<T> raw[kDeep];
+#pragma unroll
+            for (int y = 0; y < kDeep; ++y) {
+                const int r = min(r0 + y * SIDE, rows - 1), t = r / p.n_q;
+                raw[y].load(p.q + (int64_t)(t0 + t) * p.q_ts + (r - t * p.n_q) * p.q_hs, at.c0, at.c1);
+            }
+#pragma unroll
+            for (int y = 0; y < kDeep; ++y) {
+                const int r = r0 + y * SIDE, t = r / p.n_q, head = r - t * p.n_q, token = t0 + t;
+                if (r >= rows) break;                // the same for all lanes of a row
+                const int pos = place[t];
+                if (pos == 1 << 30) continue;
+                float x[16];
+                raw[y].get(x);
+                norm_turn<D>(p, at, p.q_norm ? p.q_norm + head * p.q_nhs : nullptr, p.rope ? turn_of(p, token, pos) : nullptr, x);
+                store_row<T>(p.q_out + ((int64_t)token * p.n_q + head) * (D * (int)sizeof(T)), at.c0, at.c1, x);
+            }
         }
         return;
     }
@@ -226,27 +275,40 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(NormArgs p) {
             if (EIGHT && tid < old) lc[tid] = codes[s0 + tid];
         }
         const int t0 = first + (base + s0 - p0);                     // the slab's first slot, were it new
-#pragma unroll 2
-        for (int i = a + tid / L; i < b; i += SIDE) {
-            const int token = t0 + i;
-            float x[8], y[8];
-            load_row<T>(p.k + h * p.k_hs + (int64_t)token * p.k_ts, at.c0, at.c1, x);
-            load_row<T>(p.v + h * p.v_hs + (int64_t)token * p.v_ts, at.lane * 8, at.lane * 8 + 4, y);
-            norm_turn<D>(p, at, w, at.turned ? turn_of(p, token, base + s0 + i) : nullptr, x);
-            if constexpr (EIGHT) {
-                unsigned k0, k1, kcode, v0, v1, vcode;
-                to8<D>(x, k0, k1, kcode);
-                to8<D>(y, v0, v1, vcode);
-                *(unsigned*)(lk + i * ROW + at.c0) = k0;
-                *(unsigned*)(lk + i * ROW + at.c1) = k1;
-                *(uint2*)(lv + i * ROW + at.lane * 8) = uint2{v0, v1};
-                if (at.lane == 0) {
-                    lc[i] = (uint8_t)kcode;
-                    lc[SLAB + i] = (uint8_t)vcode;
+        const int v0 = at.lane * 8, v1 = D / 2 + at.lane * 8;
+        for (int i0 = a + tid / L; i0 < b; i0 += SIDE * kDeep) {
+            Raw<T> kr[kDeep], vr[kDeep];
+#pragma unroll
+            for (int y = 0; y < kDeep; ++y) {
+                const int64_t token = t0 + min(i0 + y * SIDE, b - 1);
+                kr[y].load(p.k + h * p.k_hs + token * p.k_ts, at.c0, at.c1);
+                vr[y].load(p.v + h * p.v_hs + token * p.v_ts, v0, v1);
+            }
+#pragma unroll
+            for (int y = 0; y < kDeep; ++y) {
+                const int i = i0 + y * SIDE;
+                if (i >= b) break;
+                float x[16];
+                kr[y].get(x);
+                norm_turn<D>(p, at, w, p.rope ? turn_of(p, t0 + i, base + s0 + i) : nullptr, x);
+                if constexpr (EIGHT) {
+                    unsigned kcode, vcode;
+                    kv_u32x4 u = to8<D>(x, kcode);
+                    *(uint2*)(lk + i * ROW + at.c0) = uint2{u[0], u[1]};
+                    *(uint2*)(lk + i * ROW + at.c1) = uint2{u[2], u[3]};
+                    vr[y].get(x);
+                    u = to8<D>(x, vcode);
+                    *(uint2*)(lv + i * ROW + v0) = uint2{u[0], u[1]};
+                    *(uint2*)(lv + i * ROW + v1) = uint2{u[2], u[3]};
+                    if (at.lane == 0) {
+                        lc[i] = (uint8_t)kcode;
+                        lc[SLAB + i] = (uint8_t)vcode;
+                    }
+                } else {
+                    store_row<T>(lk + i * ROW, at.c0, at.c1, x);
+                    vr[y].get(x);
+                    store_row<T>(lv + i * ROW, v0, v1, x);
                 }
-            } else {
-                store_row<T>(lk + i * ROW, at.c0, at.c1, x);
-                store_row<T>(lv + i * ROW, at.lane * 8, at.lane * 8 + 4, y);
             }
         }
         __syncthreads();
@@ -332,7 +394,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(NormArgs p) {
     }
     if (!p.sig) return;
     __shared__ unsigned biggest[kThreads / 64];
-    __shared__ float part[8 * D];
+    float* part = (float*)lk;                        // [8][D]
+    static_assert(sizeof(lk) >= 8 * D * sizeof(float), "sums fit the slab");
 #pragma unroll
     for (int y = 0; y < SUMS; ++y)
 #pragma unroll
