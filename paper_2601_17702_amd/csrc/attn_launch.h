@@ -11,13 +11,14 @@ constexpr int s3_few_rows(bool bf16, int d_head, bool list) {
     return !bf16 ? (d_head == 128 ? 128 : 64) : list || d_head != 128 ? 64 : 32;
 }
 
-// Sequences, or tiles of listed blocks, of few rows (R: the most that one has, 128 at most); tiles: how many there can be.
+// Sequences, or tiles of listed blocks, of few rows (R: the most that one has, 128 at most); tiles: how many there can be;
+// most_tokens: a bound of what one sees.
 size_t s3_attn_stream_workspace(int d_head, int R);
-int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
+int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
 // Its builds for capped scores, for 8-bit caches (dtype kS3E4m3), and for both.
-int s3_attn_stream_cap(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
-int s3_attn_stream_8(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
-int s3_attn_stream_8_cap(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, void* ws, hipStream_t st);
+int s3_attn_stream_cap(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
+int s3_attn_stream_8(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
+int s3_attn_stream_8_cap(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
 
 // Chunks, or tiles of listed blocks, of more rows: row tiles of s3_attn_tile_rows rows, the tokens of each in n_split parts.
 int s3_attn_tile_rows(const s3_kv_cache* c);

@@ -24,7 +24,7 @@ int check_ws(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
 struct Plan {
     int G, R, qb, per_q, n_split, limit;
     bool few, many;
-    int64_t few_tiles, many_tiles;
+    int64_t few_tiles, many_tiles, few_tokens;
     size_t few_ws, many_ws;
     size_t bytes() const { return few_ws + many_ws; }
     Plan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b, int window) {
@@ -50,10 +50,12 @@ struct Plan {
         // that is not full; none has more than max_new tokens
         const int64_t all = (int64_t)b->n_tokens * G, longs = min((int64_t)min(b->n_seq, b->n_tokens), few ? all / (limit + 1) : all);
         many_tiles = !many ? 0 : q_block ? s3_block_tiles(b, q_block) * per_q : min((all + longs * (rows - 1)) / rows, longs * ((most + rows - 1) / rows));
-        const int64_t units = many_tiles * c->n_kv_heads, tokens = q_block ? (int64_t)top_b * c->page_size : b->max_kv;
+        const int64_t units = many_tiles * c->n_kv_heads;
+        const int64_t tokens = few_tokens = q_block ? (int64_t)top_b * c->page_size : b->max_kv;
         const bool ragged = !q_block && b->n_seq > 1;
         n_split = many ? s3_attn_tile_split(c, units, tokens, ragged) : 1;
         many_ws = s3_attn_tile_workspace(c, units, n_split);              // for any window
+        if (window && !q_block) few_tokens = min(tokens, (int64_t)window + R / G + 32);
         if (many && window) n_split = min(n_split, s3_attn_tile_split(c, units, min(tokens, (int64_t)window + rows / G), ragged));
     }
 };
@@ -66,7 +68,7 @@ int run(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b, AttnArgs p, 
     if (max(plan.few ? plan.few_tiles : 0, plan.many_tiles) * c->n_kv_heads >= (int64_t)1 << 22)
         return s3_fail(S3_EINVAL, "%s: %lld row tiles and %d heads are too many for one call", fn, (long long)max(plan.few_tiles, plan.many_tiles), c->n_kv_heads);
     if (plan.few)
-        if (int rc = s3_attn_stream(c, p, plan.few_tiles, plan.R, ws, st)) return rc;
+        if (int rc = s3_attn_stream(c, p, plan.few_tiles, plan.R, plan.few_tokens, ws, st)) return rc;
     return plan.many ? s3_attn_tile(c, p, plan.many_tiles, plan.n_split, (char*)ws + plan.few_ws, st) : S3_OK;
 }
 
