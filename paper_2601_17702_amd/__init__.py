@@ -139,13 +139,20 @@ def _check(rc: int):
         raise S3Error(rc, lib().s3_last_error().decode())
 
 
+_raw_stream = None
+
+
 def _stream():
     """The current stream's handle.  torch.cuda.current_stream() builds a Stream object around it, 3.2 us a call; the two
     calls it makes itself take 0.2."""
-    import torch
-    if torch.cuda.is_initialized():
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-    return torch.cuda.current_stream().cuda_stream
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        if not torch.cuda.is_initialized():
+            return torch.cuda.current_stream().cuda_stream
+        _raw_stream = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    stream, device = _raw_stream
+    return stream(device())
 
 
 def _ptr(t):
@@ -578,8 +585,9 @@ class KVCache:
             n_q = q.shape[1]
             assert q.shape[0] == T
             if q_out is None:
-                q_out = _torch().empty_like(q, memory_format=_torch().contiguous_format)
-            assert q_out.shape == q.shape and q_out.dtype is q.dtype and q_out.is_contiguous() and q_out.is_cuda
+                q_out = q.new_empty(q.shape)
+            else:
+                assert q_out.shape == q.shape and q_out.dtype is q.dtype and q_out.is_contiguous() and q_out.is_cuda
             op = q_out.data_ptr()
         norm = None
         if q_norm is not None or k_norm is not None:
@@ -603,9 +611,10 @@ class KVCache:
         if positions is not None:
             assert positions.is_cuda and positions.is_contiguous() and positions.dtype is torch.int32 and positions.shape == (n_rows,)
         shape = (n_rows, self.n_kv_heads, self.d_head)
-        k, v = (kv_len.new_empty(shape, dtype=self.dtype) if x is None else x for x in (k_out, v_out))
-        for x in (k, v):
-            assert x.is_cuda and x.is_contiguous() and x.dtype is self.dtype and x.shape == shape
+        for x in (k_out, v_out):
+            assert x is None or (x.is_cuda and x.is_contiguous() and x.dtype is self.dtype and x.shape == shape)
+        k = self.k.new_empty(shape, dtype=self.dtype) if k_out is None else k_out
+        v = self.k.new_empty(shape, dtype=self.dtype) if v_out is None else v_out
         rc = self._read(self._c, b, _ptr(positions), k.data_ptr(), v.data_ptr(), _stream())
         if rc:
             _check(rc)
@@ -623,12 +632,11 @@ class KVCache:
         return ws
 
     def _out(self, q, out, want_lse, need, ws):
-        torch = _torch()
         if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            out = q.new_empty(q.shape)
         else:
             assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.is_cuda
-        lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
+        lse = q.new_empty(q.shape[:2], dtype=_torch().float32) if want_lse else None
         return out, lse, self._scratch(q, need, ws)
 
     def _attend(self, head, scale, softcap, window, tail):

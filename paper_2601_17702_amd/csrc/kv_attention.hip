@@ -42,7 +42,6 @@ struct Plan {
         const bool all_long = b->n_tokens > (int64_t)(b->n_seq - 1) * b->max_new + limit / G;
         few = !many || (!q_block && !all_long);
         R = (int)min(most, (int64_t)limit);                    // a sequence's, or a tile of listed blocks', are one row tile
-        few_ws = few ? s3_attn_stream_workspace(c->d_head, R) : 0;
         const int rows = s3_attn_tile_rows(c);
         per_q = (int)((most + rows - 1) / rows);
         few_tiles = q_block ? s3_block_tiles(b, q_block) : min(b->n_seq, b->n_tokens);
@@ -55,6 +54,7 @@ struct Plan {
         const bool ragged = !q_block && b->n_seq > 1;
         n_split = many ? s3_attn_tile_split(c, units, tokens, ragged) : 1;
         many_ws = s3_attn_tile_workspace(c, units, n_split);              // for any window
+        few_ws = few ? s3_attn_stream_workspace(c, q_block != 0, R, few_tiles * c->n_kv_heads, tokens) : 0;      // for any window
         if (window && !q_block) few_tokens = min(tokens, (int64_t)window + R / G + 32);
         if (many && window) n_split = min(n_split, s3_attn_tile_split(c, units, min(tokens, (int64_t)window + rows / G), ragged));
     }

@@ -20,6 +20,9 @@ def norm(q=ONE, k=ONE, qs=0, ks=0, eps=1e-6):
     return s3._KV_NORM.pack(q, k, qs, ks, eps)
 
 
+LONG = dict(max_kv=4096, max_pages=64, stride=64)       # of which no workgroup takes a tile whole
+
+
 def attend(c=None, b=None, q=ONE, n_q=8, ts=1024, hs=128, scale=0.1, cap=0.0, window=0, out=ONE, ws=ONE, ws_bytes=1 << 40):
     return s3.lib().s3_kv8_attention(c or cache(), b or batch(), q, n_q, ts, hs, scale, cap, window, out, None, ws, ws_bytes, None)
 
@@ -64,11 +67,11 @@ def test_bad_arguments_of_each_call():
     nan, inf = float("nan"), float("inf")
     assert all(attend(**x) == -1 for x in (dict(q=0), dict(q=ONE + 8), dict(n_q=7), dict(n_q=0), dict(n_q=66), dict(ts=1020), dict(hs=130), dict(hs=64),
                                            dict(ts=-1024), dict(scale=0.0), dict(scale=nan), dict(scale=inf), dict(window=-1), dict(out=0), dict(out=ONE + 8),
-                                           dict(ws=0), dict(ws=ONE + 128), dict(cap=-1.0), dict(cap=nan), dict(cap=inf), dict(cap=2e30), dict(cap=1e-20, scale=1e20)))
+                                           dict(ws=0, b=batch(**LONG)), dict(ws=ONE + 128, b=batch(**LONG)), dict(cap=-1.0), dict(cap=nan), dict(cap=inf), dict(cap=2e30), dict(cap=1e-20, scale=1e20)))
     assert b"s3_kv8_attention" in s3.lib().s3_last_error()
-    assert attend(ws_bytes=16) == -3
-    assert all(listed(**x) == -1 for x in (dict(sel=0), dict(q_block=0), dict(top=0), dict(top=4097), dict(n_q=3), dict(ws=0, q_block=4), dict(cap=-0.5)))
-    assert listed(ws_bytes=16, q_block=4) == -3
+    assert attend(ws_bytes=16, b=batch(**LONG)) == -3
+    assert all(listed(**x) == -1 for x in (dict(sel=0), dict(q_block=0), dict(top=0), dict(top=4097), dict(n_q=3), dict(ws=0, q_block=4, top=40), dict(cap=-0.5)))
+    assert listed(ws_bytes=16, q_block=4, top=40) == -3
     assert all(capped(**x) == -1 for x in (dict(cap=0.0), dict(cap=-1.0), dict(cap=nan), dict(cap=inf), dict(window=-1), dict(ws=0), dict(scale=0.0)))
     assert capped(ws_bytes=16) == -3
     L = s3.lib()
@@ -97,8 +100,20 @@ def test_nothing_to_do():
 def test_sizes():
     assert s3._KV8_CACHE.size == 48 and s3._KV_NORM.size == 40 and C.sizeof(C.c_void_p) == 8
     L = s3.lib()
-    for b, n_q in ((batch(), 8), (batch(n_tokens=600, max_new=600), 32), (batch(qs=0, n_tokens=2, max_new=1), 8)):
+    for b, n_q in ((batch(n_tokens=600, max_new=600), 32), (batch(qs=0, n_tokens=2, max_new=1, max_kv=2000, max_pages=32, stride=32), 8)):
         assert L.s3_kv8_attention_workspace(cache(), b, n_q) == L.s3_paged_attention_workspace(cache16(), b, n_q) > 0
+
+
+def test_scratch_of_tiles_that_one_workgroup_has():
+    """None, where nothing is joined: few rows, and a bound of 1024 tokens, or of 2048 and a workgroup for every compute unit (lists: 8192)."""
+    def need(n_seq, max_kv, max_new=1, heads=8, n_q=32):
+        pages = -(-max_kv // 64)
+        b = batch(qs=0 if max_new == 1 else ONE, n_seq=n_seq, n_tokens=n_seq * max_new, max_new=max_new, max_pages=pages, stride=pages, max_kv=max_kv)
+        return s3.lib().s3_kv8_attention_workspace(cache(heads=heads), b, n_q)
+    assert need(1, 1024) == need(32, 2048) == need(1, 1000, max_new=4) == 0
+    assert need(1, 1025) > 0 and need(31, 2048) > 0 and need(64, 2049) > 0 and need(1, 1000, max_new=5) > 0
+    lists = lambda top, n_seq: s3.lib().s3_kv8_block_attention_workspace(cache(heads=8), batch(qs=0, n_seq=n_seq, n_tokens=n_seq, max_new=1), 32, 1, top)  # noqa: E731
+    assert lists(16, 1) == lists(128, 32) == 0 and lists(17, 1) > 0 and lists(129, 32) > 0
 
 
 def test_plain_form_of_8_bits():
