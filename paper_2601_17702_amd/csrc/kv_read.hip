@@ -1,13 +1,13 @@
 // Tokens of a paged cache back as rows (s3_kv_read, s3_kv8_read).
 //
-// What bounds it: memory.  A workgroup has 64 rows of one head.  Of the keys a lane takes a row's 16-byte piece and eight rows' lie in one line; the
+// What bounds it: memory.  A workgroup has 32 rows of one head.  Of the keys a lane takes a row's 16-byte piece and eight rows' lie in one line; the
 // values' pieces hold E tokens of a channel, so the rows' groups of E tokens are turned over through LDS, each group once
 // for all consecutive rows that lie in it (rows in ascending order, as evidence spans are, read every line once).
 #include "kv_cache.h"
 
 namespace {
 
-constexpr int kThreads = 256, kRows = 64;
+constexpr int kThreads = 256, kRows = 32;
 
 struct ReadArgs {
     KvBatch b;
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs p) {
     const int logp = p.b.log_page, P = 1 << logp;
     const int n_rows = min(kRows, p.b.n_tokens - t0);
 
-    if (tid < kRows) {                                  // where the rows lie: a page, -1 (zeros) or -2 (of no sequence)
+    if (tid < 64) {                                     // where the rows lie: a page, -1 (zeros) or -2 (of no sequence)
         const int token = t0 + tid;
         int s = t0;
         if (p.b.q_start) {                              // the first sequence that ends behind the first row
@@ -60,15 +60,57 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs p) {
         const bool begins = page >= 0 && (tid == 0 || page != before_page || group != before_group);
         const uint64_t all = __ballot(begins);
         const int mine = __popcll(all & (~(uint64_t)0 >> (63 - tid))) - 1;
-        pages[tid] = page;
-        slots[tid] = slot;
-        group_of[tid] = page >= 0 ? mine : -1;
+        if (tid < kRows) {
+            pages[tid] = page;
+            slots[tid] = slot;
+            group_of[tid] = page >= 0 ? mine : -1;
+        }
         if (begins) groups[mine] = tid;                 // a row of it
         if (tid == 0) n_groups = __popcll(all);
     }
     __syncthreads();
     const int64_t page_bytes = (int64_t)P * D * ES;
 
+    // A thread's pieces of some groups: of one channel, or of 8 bits of four, whose 4 x 4 squares of bytes are turned.  The first groups' are on
+    // their way while the keys are read.
+    constexpr int CH = EIGHT ? 4 : 1, ITEMS = (GROUPS * (D / CH) + kThreads - 1) / kThreads;
+    kv_u32x4 x[ITEMS][CH];
+    auto load = [&](int g0, int ng) {
+#pragma unroll
+        for (int y = 0; y < ITEMS; ++y) {
+            const int i = tid + y * kThreads;
+            if (i >= ng * (D / CH)) break;
+            const int g = i / (D / CH), c = i % (D / CH) * CH, r = groups[g0 + g];
+            const char* src = p.vc + ((int64_t)pages[r] * p.n_kv + h) * page_bytes + ((int64_t)(slots[r] / E) * D + c) * 16;
+#pragma unroll
+            for (int z = 0; z < CH; ++z) x[y][z] = *(const kv_u32x4*)(src + z * 16);
+        }
+    };
+    auto turn = [&](int ng) {
+#pragma unroll
+        for (int y = 0; y < ITEMS; ++y) {
+            const int i = tid + y * kThreads;
+            if (i >= ng * (D / CH)) break;
+            const int g = i / (D / CH), c = i % (D / CH) * CH;
+            if constexpr (EIGHT) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned a0 = __builtin_amdgcn_perm(x[y][1][e], x[y][0][e], 0x05010400u), a1 = __builtin_amdgcn_perm(x[y][1][e], x[y][0][e], 0x07030602u);
+                    const unsigned b0 = __builtin_amdgcn_perm(x[y][3][e], x[y][2][e], 0x05010400u), b1 = __builtin_amdgcn_perm(x[y][3][e], x[y][2][e], 0x07030602u);
+                    char* dst = turned + (g * E + e * 4) * ROW + c;
+                    *(unsigned*)dst = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+                    *(unsigned*)(dst + ROW) = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+                    *(unsigned*)(dst + 2 * ROW) = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+                    *(unsigned*)(dst + 3 * ROW) = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+                }
+            } else {
+                const typename KvElem<T>::vec v = __builtin_bit_cast(typename KvElem<T>::vec, x[y][0]);
+#pragma unroll
+                for (int e = 0; e < E; ++e) *(T*)(turned + (g * E + e) * ROW + c * ES) = v[e];
+            }
+        }
+    };
+    if (p.v) load(0, min(GROUPS, n_groups));
     if (p.k)
         for (int i = tid; i < n_rows * NG; i += kThreads) {
             const int r = i / NG, g = i % NG, page = pages[r];
@@ -99,32 +141,8 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs p) {
     constexpr int OUT = 16 / (int)sizeof(T);            // channels of a store
     for (int g0 = 0; g0 == 0 || g0 < n_groups; g0 += GROUPS) {
         const int ng = min(GROUPS, n_groups - g0);
-        if constexpr (EIGHT) {                          // four channels' pieces: 4 x 4 squares of bytes are turned
-            for (int i = tid; i < ng * (D / 4); i += kThreads) {
-                const int g = i / (D / 4), c = i % (D / 4) * 4, r = groups[g0 + g];
-                const char* src = p.vc + ((int64_t)pages[r] * p.n_kv + h) * page_bytes + ((int64_t)(slots[r] / E) * D + c) * 16;
-                kv_u32x4 x[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) x[y] = *(const kv_u32x4*)(src + y * 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const unsigned a0 = __builtin_amdgcn_perm(x[1][e], x[0][e], 0x05010400u), a1 = __builtin_amdgcn_perm(x[1][e], x[0][e], 0x07030602u);
-                    const unsigned b0 = __builtin_amdgcn_perm(x[3][e], x[2][e], 0x05010400u), b1 = __builtin_amdgcn_perm(x[3][e], x[2][e], 0x07030602u);
-                    char* dst = turned + (g * E + e * 4) * ROW + c;
-                    *(unsigned*)dst = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
-                    *(unsigned*)(dst + ROW) = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
-                    *(unsigned*)(dst + 2 * ROW) = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
-                    *(unsigned*)(dst + 3 * ROW) = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
-                }
-            }
-        } else {
-            for (int i = tid; i < ng * D; i += kThreads) {
-                const int g = i / D, c = i % D, r = groups[g0 + g];
-                const typename KvElem<S>::vec x = *(const typename KvElem<S>::vec*)(p.vc + ((int64_t)pages[r] * p.n_kv + h) * page_bytes + ((int64_t)(slots[r] / E) * D + c) * 16);
-#pragma unroll
-                for (int e = 0; e < E; ++e) *(S*)(turned + (g * E + e) * ROW + c * ES) = x[e];
-            }
-        }
+        if (g0) load(g0, ng);
+        turn(ng);
         __syncthreads();
         for (int i = tid; i < n_rows * (D / OUT); i += kThreads) {
             const int r = i / (D / OUT), c = i % (D / OUT) * OUT, page = pages[r], g = group_of[r] - g0;
