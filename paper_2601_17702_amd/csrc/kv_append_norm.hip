@@ -322,19 +322,19 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(NormArgs p) {
                 const int slot = tid & (SLAB - 1), which = tid / SLAB;
                 if (slot >= a && slot < b) codes[which * P + s0 + slot] = lc[which * SLAB + slot];
             }
-            // E slots of one channel (8 bits: of four channels, whose 4 x 4 squares of bytes are turned)
+            // whole groups of E slots: of one channel (8 bits: of four, whose 4 x 4 squares of bytes are turned); then the slots of groups that are partly new
             constexpr int CH = EIGHT ? 4 : 1;
-            for (int i = tid; i < ((b + E - 1) / E - a / E) * (D / CH); i += kThreads) {
-                const int c = i % (D / CH) * CH, g = a / E + i / (D / CH);
+            const int ga = (a + E - 1) / E, gb = b / E;
+            for (int i = tid; i < (gb - ga) * (D / CH); i += kThreads) {
+                const int c = i % (D / CH) * CH, g = ga + i / (D / CH);
                 char* dst = vp + ((int64_t)(s0 / E + g) * D + c) * 16;
-                const bool whole = g * E >= a && g * E + E <= b;
                 if constexpr (EIGHT) {
                     kv_u32x4 x[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         unsigned u[4];
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) u[r] = *(const unsigned*)(lv + (g * E + e * 4 + r) * ROW + c);      // of other slots: not stored
+                        for (int r = 0; r < 4; ++r) u[r] = *(const unsigned*)(lv + (g * E + e * 4 + r) * ROW + c);
                         const unsigned a0 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), a1 = __builtin_amdgcn_perm(u[1], u[0], 0x07030602u);
                         const unsigned b0 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u), b1 = __builtin_amdgcn_perm(u[3], u[2], 0x07030602u);
                         x[0][e] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
@@ -343,27 +343,18 @@ __global__ __launch_bounds__(kThreads) void kv_append_norm_kernel(NormArgs p) {
                         x[3][e] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
                     }
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        if (whole) {
-                            *(kv_u32x4*)(dst + y * 16) = x[y];
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (g * E + e >= a && g * E + e < b) dst[y * 16 + e] = (char)(x[y][e / 4] >> (e % 4 * 8));
-                        }
-                    }
+                    for (int y = 0; y < 4; ++y) *(kv_u32x4*)(dst + y * 16) = x[y];
                 } else {
-                    typename KvElem<S>::vec x;
+                    typename KvElem<T>::vec x;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = *(const S*)(lv + (g * E + e) * ROW + c * ES);
-                    if (whole) {
-                        *(typename KvElem<S>::vec*)dst = x;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            if (g * E + e >= a && g * E + e < b) ((S*)dst)[e] = x[e];
-                    }
+                    for (int e = 0; e < E; ++e) x[e] = *(const T*)(lv + (g * E + e) * ROW + c * ES);
+                    *(typename KvElem<T>::vec*)dst = x;
                 }
+            }
+            const int before = ga <= gb ? ga * E - a : fresh, part = before + (ga <= gb ? b - gb * E : 0);
+            for (int i = tid; i < part * D; i += kThreads) {
+                const int k = i / D, c = i % D, slot = k < before ? a + k : gb * E + (k - before);
+                *(S*)(vp + ((int64_t)(s0 + slot) / E * D + c) * 16 + slot % E * ES) = *(const S*)(lv + slot * ROW + c * ES);
             }
         }
         if (p.sig) {
