@@ -550,18 +550,20 @@ class KVCache:
         return _KV_BATCH.pack(qs, kv_len.data_ptr(), block_table.data_ptr(), stride if rows > 1 else width, n_seq, n_tokens, width,
                               n_tokens if max_new is None else max_new, width * self.page_size if max_kv is None else max_kv)
 
-    def _rows(self, x, heads=None):
-        _, n, d = x.shape
+    def _rows(self, x, tokens, heads=None):
+        T, n, d = x.shape
         ts, hs, inner = x.stride()
-        assert x.dtype is self.dtype and x.is_cuda and d == self.d_head and inner == 1 and (heads is None or n == heads)
-        return x.data_ptr(), ts, hs
+        assert x.dtype is self.dtype and x.is_cuda and d == self.d_head and inner == 1 and T == tokens and (heads is None or n == heads)
+        return x.data_ptr(), ts, hs, n
 
     def _weights(self, w, heads):
         """A norm's weights, [d_head] for all heads or [heads, d_head]: address, and from head to head."""
         if w is None:
             return 0, 0
-        assert w.is_cuda and w.dtype is _torch().float32 and w.is_contiguous() and w.shape in ((self.d_head,), (heads, self.d_head))
-        return w.data_ptr(), self.d_head if w.dim() == 2 else 0
+        d = self.d_head
+        each = w.dim() == 2
+        assert w.is_cuda and w.dtype is _torch().float32 and w.is_contiguous() and w.shape == ((heads, d) if each else (d,))
+        return w.data_ptr(), d if each else 0
 
     def append(self, k, v, kv_len, block_table, q_start=None, rope=None, interleaved: bool = False, positions=None, q=None, q_out=None,
                max_new=None, q_norm=None, k_norm=None, eps: float = 1e-6):
@@ -569,9 +571,8 @@ class KVCache:
         or k_norm (fp32 weights, [d_head] or [heads, d_head]) s3_kv_append_norm: rows over the root of their mean square plus eps, before the
         rotation.  Returns the rotated q, or None without q."""
         T = k.shape[0]
-        kp, kt, kh = self._rows(k, self.n_kv_heads)
-        vp, vt, vh = self._rows(v, self.n_kv_heads)
-        assert v.shape[0] == T
+        kp, kt, kh, heads = self._rows(k, T, self.n_kv_heads)
+        vp, vt, vh, _ = self._rows(v, T, heads)
         b = self._batch(T, kv_len, block_table, q_start, max_new, None)
         rp = n_pos = rot = n_q = qp = qt = qh = op = 0
         if rope is not None:
@@ -581,9 +582,7 @@ class KVCache:
         if positions is not None:
             assert positions.is_cuda and positions.is_contiguous() and positions.dtype is kv_len.dtype and positions.shape == (T,)
         if q is not None:
-            qp, qt, qh = self._rows(q)
-            n_q = q.shape[1]
-            assert q.shape[0] == T
+            qp, qt, qh, n_q = self._rows(q, T)
             if q_out is None:
                 q_out = q.new_empty(q.shape)
             else:
@@ -592,7 +591,7 @@ class KVCache:
         norm = None
         if q_norm is not None or k_norm is not None:
             assert q_norm is None or q is not None
-            (qw, qs), (kw, ks) = self._weights(q_norm, n_q), self._weights(k_norm, self.n_kv_heads)
+            (qw, qs), (kw, ks) = self._weights(q_norm, n_q), self._weights(k_norm, heads)
             norm = _KV_NORM.pack(qw, kw, qs, ks, eps)
         rc = self._append((self._c, b, kp, kt, kh, vp, vt, vh, rp, n_pos, rot, interleaved, _ptr(positions), qp, n_q, qt, qh, op), norm)
         if rc:
@@ -661,7 +660,7 @@ class KVCache:
         s3_paged_attention_capped: scores softcap * tanh(score / softcap).  Returns (out, lse fp32 [n_tokens, n_q_heads] | None)."""
         T, n_q, _ = q.shape
         b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
-        qp, qt, qh = self._rows(q)
+        qp, qt, qh, _ = self._rows(q, T)
         need = self._attend_workspace(self._c, b, n_q)
         out, lse, ws = self._out(q, out, want_lse, need, ws)
         rc = self._attend((self._c, b, qp, n_q, qt, qh), self.scale if scale is None else scale, softcap, window,
@@ -677,7 +676,7 @@ class KVCache:
         torch = _torch()
         T, n_q, _ = q.shape
         b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
-        qp, qt, qh = self._rows(q)
+        qp, qt, qh, _ = self._rows(q, T)
         sel = q.new_empty((_lib.s3_block_tiles(b, q_block), self.n_kv_heads, top_b), dtype=torch.int32)
         need = _lib.s3_block_select_workspace(self._c16, b, n_q, q_block, top_b)
         ws = self._scratch(q, need, ws)
@@ -693,7 +692,7 @@ class KVCache:
         evidence spans).  Returns (out, lse | None)."""
         T, n_q, _ = q.shape
         b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
-        qp, qt, qh = self._rows(q)
+        qp, qt, qh, _ = self._rows(q, T)
         tiles, heads, top_b = sel.shape
         assert sel.is_cuda and sel.is_contiguous() and sel.dtype is kv_len.dtype and heads == self.n_kv_heads
         assert tiles >= _lib.s3_block_tiles(b, q_block)
