@@ -254,28 +254,28 @@ struct AttnState {
 // 1 - 2 / (1 + exp(2 z)).  Where all of a wavefront's are small, as a cap well above the scores leaves them, only the series runs.
 // us with the second / with the first, chunks of 333, 826 and 2048 tokens that see 4096 each, 32 heads over 8, bf16: 484 / 342.
 constexpr float kS3NearCap = 2048.0f;
-template <int N>
-__device__ __forceinline__ void kv_cap_near(kv_f32x16 (&s)[N], const AttnArgs& p) {
+template <typename V, int N>
+__device__ __forceinline__ void kv_cap_near(V (&s)[N], const AttnArgs& p) {
     const float k = -2.8853900817779268f * p.to_cap;
 #pragma unroll
     for (int x = 0; x < N; ++x)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[x][i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[x][i] * k));
+        for (int i = 0; i < (int)(sizeof(V) / 4); ++i) s[x][i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[x][i] * k));
 }
 __device__ __forceinline__ bool kv_near(const AttnArgs& p) { return p.cap_lse != 0.0f; }
-template <int N>
-__device__ __forceinline__ void kv_cap_far(kv_f32x16 (&s)[N], const AttnArgs& p) {
+template <typename V, int N>
+__device__ __forceinline__ void kv_cap_far(V (&s)[N], const AttnArgs& p) {
     const float u = p.to_cap, c = p.cap;
     float most = 0.0f;
 #pragma unroll
     for (int x = 0; x < N; ++x)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(s[x][i]));
+        for (int i = 0; i < (int)(sizeof(V) / 4); ++i) most = fmaxf(most, fabsf(s[x][i]));
     const bool some = __ballot(!(most * u < 0.35f)) != 0;
 #pragma unroll
     for (int x = 0; x < N; ++x)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < (int)(sizeof(V) / 4); ++i) {
             const float z = s[x][i] * u, w = z * z;
             const float small = z * c * fmaf(w, fmaf(w, fmaf(w, fmaf(w, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
             if (some) {
@@ -288,8 +288,8 @@ __device__ __forceinline__ void kv_cap_far(kv_f32x16 (&s)[N], const AttnArgs& p)
         }
 }
 
-template <bool BF16, int N>
-__device__ __forceinline__ void kv_cap(kv_f32x16 (&s)[N], const AttnArgs& p) {
+template <bool BF16, typename V, int N>
+__device__ __forceinline__ void kv_cap(V (&s)[N], const AttnArgs& p) {
     if (BF16 && kv_near(p)) kv_cap_near(s, p);
     else kv_cap_far(s, p);
 }

@@ -11,12 +11,13 @@ constexpr int s3_few_rows(bool bf16, int d_head, bool list) {
     return !bf16 ? (d_head == 128 ? 128 : 64) : list || d_head != 128 ? 64 : 32;
 }
 
-// Over an 8-bit cache 16 rows are a tile of their own, and whether one workgroup takes all tokens of such a tile and head, which saves the joining launch, or the
+// Over an 8-bit cache, and with capped scores over one of bf16, 16 rows are a tile of their own, and whether one workgroup takes all tokens of such a tile and head, which saves the joining launch, or the
 // line is cut in equal runs, goes by the bound that the host knows: the longest tile alone takes 4 us and 1 us for every 256 tokens.  us whole / cut, 8 heads of 128: one
 // sequence of 512 7.0 / 11.1, of 1024 9.1 / 11.2, of 2048 13.3 / 11.3; 8 of 1024 9.4 / 11.5, of 2048 15.9 / 14.3; 64 of 512 15.3 / 21.9, of 2048 43 / 50; 256 of 2048
 // 186 / 213.  Lists are about as long as one another, so for those more; lengths beyond 2048 may lie far apart, and one of 8192 among short ones would take 39 alone.
-constexpr bool s3_whole_tiles(bool eight, bool list, int R, int64_t units, int64_t tokens) {
-    return eight && R <= 16 && (tokens <= 1024 || (units >= 256 && tokens <= (list ? 8192 : 2048)));
+constexpr bool s3_has_tiles16(bool eight, bool bf16, bool cap) { return eight || (bf16 && cap); }
+constexpr bool s3_whole_tiles(int R, bool list, int64_t units, int64_t tokens) {
+    return R <= 16 && (tokens <= 1024 || (units >= 256 && tokens <= (list ? 8192 : 2048)));
 }
 
 // Sequences, or tiles of listed blocks, of few rows (R: the most that one has, 128 at most); tiles: how many there can be;

@@ -2,7 +2,7 @@
 #include "attn_stream_impl.inc"
 
 size_t s3_attn_stream_workspace(const s3_kv_cache* c, bool list, int R, int64_t units, int64_t most_tokens) {
-    return s3_whole_tiles(c->dtype == kS3E4m3, list, R, units, most_tokens) ? 0 : s3_align((size_t)kRunGroups * 2 * slot_floats(R, c->d_head) * 4);
+    return c->dtype == kS3E4m3 && s3_whole_tiles(R, list, units, most_tokens) ? 0 : s3_align((size_t)kRunGroups * 2 * slot_floats(R, c->d_head) * 4);
 }
 
 int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st) {
