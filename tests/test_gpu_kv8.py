@@ -154,6 +154,116 @@ def test_capped_blocks():
         paged.check(pr, o, lse, paged8.attend(pr, 5.0, sel=sel, qb=16))
 
 
+@pytest.mark.parametrize("dtype,cap", [("e4m3", 0.0), ("e4m3", 20.0), ("bf16", 20.0)])
+@pytest.mark.parametrize("n_seq,hkv,longest,window", [(40, 8, 2048, 0), (40, 8, 2049, 0), (3, 2, 1024, 0), (3, 2, 1025, 0), (33, 8, 4000, 300)])
+def test_tiles_that_one_workgroup_has_and_that_are_cut(dtype, cap, n_seq, hkv, longest, window):
+    """Both sides of the rule that gives a tile's tokens to one workgroup: few tokens, or some more and many tiles; lengths from none to the bound."""
+    rng = np.random.default_rng(n_seq + longest)
+    kv = [longest, 0, 1] + [int(x) for x in rng.integers(1, longest // 8, n_seq - 3)]
+    pr = paged8.problem(dtype, n_seq + longest, 64, 64, 2 * hkv, hkv, [1] * n_seq, kv)
+    kv_len, table = pr.args()
+    o, lse = pr.cache().attention(pr.q.cuda(), kv_len, table, max_kv=longest, window=window, softcap=cap, want_lse=True)
+    paged.check(pr, o, lse, paged8.attend(pr, cap, window=window) if cap else paged.attend(pr, window=window))
+
+
+@pytest.mark.parametrize("listed", [False, True])
+@pytest.mark.parametrize("dtype,new,G,n_seq,cap", [("e4m3", 1, 4, 1200, 0.0), ("e4m3", 1, 4, 1, 0.0), ("e4m3", 8, 4, 200, 0.0), ("e4m3", 64, 4, 100, 0.0), ("e4m3", 70, 4, 1, 5.0),
+                                                   ("bf16", 1, 4, 1200, 5.0), ("bf16", 64, 4, 3, 5.0)])
+def test_many_sequences_over_the_same_pages(dtype, new, G, n_seq, cap, listed):
+    """More work a workgroup than it looks up pages and scales for at a time, few rows and many: every sequence has the same answer."""
+    kv, P = 20000, 64
+    pr = paged8.problem(dtype, n_seq + new, 64, P, G, 1, [new], [kv])
+    n_blocks = -(-kv // P)
+    sel = np.arange(n_blocks, dtype=np.int32).reshape(1, 1, n_blocks) if listed else None
+    want = paged8.attend(pr, cap, sel=sel, qb=new if listed else None) if cap else paged.attend(pr, sel=sel, qb=new if listed else None)
+    q = pr.q.cuda().repeat(n_seq, 1, 1)
+    kv_len = torch.full((n_seq,), kv, dtype=torch.int32, device="cuda")
+    table = pr.table.cuda().repeat(n_seq, 1)
+    qs = torch.arange(n_seq + 1, dtype=torch.int32, device="cuda") * new
+    c = pr.cache()
+    if listed:
+        tiles = (n_seq * new + n_seq * (new - 1)) // new
+        dev = torch.from_numpy(sel).cuda().repeat(tiles, 1, 1)
+        o, lse = c.block_attention(q, kv_len, table, dev, q_start=qs, q_block=new, softcap=cap, want_lse=True)
+    else:
+        o, lse = c.attention(q, kv_len, table, q_start=qs, max_new=new, max_kv=kv, softcap=cap, want_lse=True)
+    o, lse = o.view(n_seq, new, G, 64), lse.view(n_seq, new, G)
+    for s in {0, n_seq // 2, n_seq - 1}:
+        paged.check(pr, o[s], lse[s], want)
+    tol = want[2].cuda().to(torch.float32) * 2
+    assert torch.all((o.float() - o[:1].float()).abs() <= tol)
+
+
+@pytest.mark.parametrize("dtype,cap", [("e4m3", 0.0), ("bf16", 9.0)])
+@pytest.mark.parametrize("n_seq,top", [(40, 140), (40, 60), (2, 60), (2, 16)])
+def test_lists_of_single_tokens(dtype, cap, n_seq, top):
+    """Lists that a workgroup takes whole and that are cut, with holes, repeats and blocks past the end."""
+    rng = np.random.default_rng(top + n_seq)
+    kv = [int(x) for x in rng.integers(1, 3000, n_seq)]
+    pr = paged8.problem(dtype, top, 64, 64, 16, 8, [1] * n_seq, kv)
+    sel = rng.integers(-1, 50, (n_seq, 8, top)).astype(np.int32)
+    sel[0, 0] = -1
+    sel[-1, -1, 3:] = -1
+    kv_len, table = pr.args()
+    o, lse = pr.cache().block_attention(pr.q.cuda(), kv_len, table, torch.from_numpy(sel).cuda(), softcap=cap, want_lse=True)
+    paged.check(pr, o, lse, paged8.attend(pr, cap, sel=sel, qb=1) if cap else paged.attend(pr, sel=sel, qb=1))
+
+
+@pytest.mark.parametrize("dtype,new,cap", [("e4m3", 1, 0.0), ("e4m3", 3, 7.0), ("e4m3", 100, 0.0), ("bf16", 2, 7.0), ("bf16", 100, 7.0), ("fp32", 70, 7.0)])
+def test_nan_far_back_and_in_the_last_block(dtype, new, cap):
+    """In a context of several batches of pages: a value that all rows see, one that only the last row sees, one that a window hides from the first rows."""
+    n, window = 30000, 29990
+    pr = paged8.problem(dtype, 21, 64, 16, 4, 2, [new], [n])
+    spots = [(12000, 0, 5), (n - 1, 1, 9), (n - new - window + 3, 1, 60)]
+    for p, h, c in spots:
+        pr.rows_v[0][p, h, c] = float("nan")
+        if dtype == "e4m3":
+            pr.bytes["v"][0][p, h, c] = 0x7f
+    o, lse = run(pr, pr.cache(), softcap=cap, window=window, max_new=new, max_kv=n)
+    out, l64, tol, ltol = paged8.attend(pr, cap, window=window) if cap else paged.attend(pr, window=window)
+    o = o.cpu().to(torch.float64)
+    assert torch.isnan(out).any() and torch.equal(torch.isnan(o), torch.isnan(out))
+    fin = torch.isfinite(out)
+    assert torch.all((o - out).abs()[fin] <= tol[fin])
+
+
+@pytest.mark.parametrize("new", [1, 6, 90])
+def test_codes_that_no_append_writes(new):
+    """0 counts as 1, and all from 248 on as 247, in attention and when read back."""
+    pr = paged8.Problem8(22, 64, 16, 4, 2, [new], [200])
+    for name in "kv":
+        pr.bytes[name][0] &= 0x87                                     # small values: nothing overflows
+    ends = np.random.default_rng(22).integers(0, 2, (200, 2)).astype(bool)
+    outs = []
+    for low, high in ((1, 247), (0, 250), (0, 255)):
+        pr.codes["v"][0][:] = np.where(ends, low, high)
+        pr.codes["k"][0][:] = np.where(ends, low, 120)
+        c = pr.cache()
+        kv_len, table = pr.args()
+        outs.append((*run(pr, c), *c.read(kv_len, table, 200, q_start=torch.tensor([0, 200], dtype=torch.int32, device="cuda"))))
+    for other in outs[1:]:
+        for a, b in zip(outs[0], other):
+            assert torch.equal(a, b)
+
+
+def test_two_calls_at_once():
+    """On two streams, with a workspace each: as one after the other."""
+    pr = paged8.Problem8(23, 128, 64, 8, 2, [1, 1, 90], [3000, 70, 500])
+    c = pr.cache()
+    kv_len, table = pr.args()
+    q, qs = pr.q.cuda(), pr.q_start.cuda()
+    want = c.attention(q, kv_len, table, q_start=qs)[0]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(5):
+        for st in streams:
+            with torch.cuda.stream(st):
+                outs.append(c.attention(q, kv_len, table, q_start=qs)[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
 # ------------------------------------------------------------------------------------------------ append
 def appended(pr, dtype, k, v, q, rope, inter, q_norm, k_norm, eps, positions, sig, before):
     """What the cache (arrays of `before` as numpy) and q_out hold after the append, in fp32 steps."""
