@@ -6,7 +6,10 @@
   answer    token by token: append, then attention over the spans' blocks, the first block and the newest ones (one
             list for all heads), and over the blocks that each step's own queries choose by the pages' signatures
 
-Run with `python examples/paged_answer.py`.  Activations are random with some structure: no weights are needed.  What is printed is the
+With eight_bits the cache is one of 8 bits, keys and queries are normed for each head on the way in, scores are capped, and at the end the spans' tokens are
+read back into a small cache of their own, whose attention needs nothing of the large one.
+
+Run with `python examples/paged_answer.py` (`--eight-bits`).  Activations are random with some structure: no weights are needed.  What is printed is the
 share of the full attention's weight that each kind of list holds, from the log-sum-exps of the three calls.
 """
 from __future__ import annotations
@@ -37,7 +40,8 @@ def span_blocks(starts, span_len: int, page: int, last_block: int, top: int, dev
 
 
 def run(context: int = 8192, chunk: int = 2048, answer: int = 8, n_q: int = 32, n_kv: int = 8, d: int = 128, page: int = 64,
-        n_feat: int = 4096, k: int = 32, top_blocks: int = 32, span: int = 64, n_spans: int = 12, seed: int = 0, device="cuda"):
+        n_feat: int = 4096, k: int = 32, top_blocks: int = 32, span: int = 64, n_spans: int = 12, seed: int = 0, device="cuda",
+        eight_bits: bool = False, softcap: float = 30.0):
     g = torch.Generator(device=device).manual_seed(seed)
     bf = torch.bfloat16
 
@@ -58,7 +62,12 @@ def run(context: int = 8192, chunk: int = 2048, answer: int = 8, n_q: int = 32, 
 
     total = context + answer
     pages = -(-total // page)
-    cache = s3.KVCache(pages, page, n_kv, d, bf, signatures=True, device=device)
+    if eight_bits:
+        cache = s3.KVCache8(pages, page, n_kv, d, signatures=True, device=device)
+        norms = {"q_norm": 1.0 + 0.1 * normal(d), "k_norm": 1.0 + 0.1 * normal(d)}
+        capped = {"softcap": softcap}
+    else:
+        cache, norms, capped = s3.KVCache(pages, page, n_kv, d, bf, signatures=True, device=device), {}, {}
     table = torch.randperm(pages, generator=g, device=device).to(torch.int32)[None]
     rope = s3.rope_table(total, d, device=device)
     w_enc = torch.nn.functional.normalize(normal(n_kv, n_feat, d), dim=-1).to(bf)
@@ -73,8 +82,8 @@ def run(context: int = 8192, chunk: int = 2048, answer: int = 8, n_q: int = 32, 
         q, keys, v = qkv[:, :n_q], qkv[:, n_q:n_q + n_kv], qkv[:, n_q + n_kv:]
         kv_len = torch.tensor([c0 + n], dtype=torch.int32, device=device)
         q_start = torch.tensor([0, n], dtype=torch.int32, device=device)
-        q = cache.append(keys, v, kv_len, table, q_start=q_start, rope=rope, q=q)
-        hidden, _ = cache.attention(q, kv_len, table, q_start=q_start, max_new=n, max_kv=c0 + n)
+        q = cache.append(keys, v, kv_len, table, q_start=q_start, rope=rope, q=q, **norms)
+        hidden, _ = cache.attention(q, kv_len, table, q_start=q_start, max_new=n, max_kv=c0 + n, **capped)
         ids, _ = s3.sae_encode_topk_stream(keys.transpose(0, 1).contiguous(), w_enc, b_enc, k, tau)
         index.append(ids, base_pos=c0)
     index.finalize()
@@ -91,20 +100,35 @@ def run(context: int = 8192, chunk: int = 2048, answer: int = 8, n_q: int = 32, 
         qkv = project(1, torch.full((1,), 5, device=device))
         length = context + t + 1
         kv_len = torch.tensor([length], dtype=torch.int32, device=device)
-        q = cache.append(qkv[:, n_q:n_q + n_kv], qkv[:, n_q + n_kv:], kv_len, table, rope=rope, q=qkv[:, :n_q])
-        full, lse = cache.attention(q, kv_len, table, max_kv=length, want_lse=True)
+        q = cache.append(qkv[:, n_q:n_q + n_kv], qkv[:, n_q + n_kv:], kv_len, table, rope=rope, q=qkv[:, :n_q], **norms)
+        full, lse = cache.attention(q, kv_len, table, max_kv=length, want_lse=True, **capped)
         last = (length - 1) // page
         named = span_blocks(starts, span, page, last, top_blocks, device).expand(1, n_kv, top_blocks).contiguous()
-        _, lse_named = cache.block_attention(q, kv_len, table, named, want_lse=True)
+        _, lse_named = cache.block_attention(q, kv_len, table, named, want_lse=True, **capped)
         chosen = cache.select(q, kv_len, table, top_blocks, lead=1, tail=2, max_kv=length)
-        _, lse_chosen = cache.block_attention(q, kv_len, table, chosen, want_lse=True)
+        _, lse_chosen = cache.block_attention(q, kv_len, table, chosen, want_lse=True, **capped)
         shares["span_share"].append(torch.exp(lse_named - lse).mean())
         shares["chosen_share"].append(torch.exp(lse_chosen - lse).mean())
-    return {"hidden": hidden, "full": full, "starts": starts, "named": named, "chosen": chosen, "blocks": last + 1,
+    kept = {}
+    if eight_bits:
+        # the evidence alone: the spans' tokens, rotated as they are, in a cache of their own
+        lo = starts.clamp(min=0)
+        _, idx, n_out = s3.fuse_indices(context, lo, torch.where(starts < 0, lo - 1, torch.clamp(lo + span - 1, max=context - 1)), None, lead=1)
+        n = int(n_out)
+        k, v = cache.read(kv_len, table, n, q_start=torch.tensor([0, n], dtype=torch.int32, device=device), positions=idx[:n])
+        small = s3.KVCache8(-(-n // page), page, n_kv, d, device=device)
+        small_table = torch.arange(small.n_pages, dtype=torch.int32, device=device)[None]
+        small_len = torch.tensor([n], dtype=torch.int32, device=device)
+        small.append(k, v, small_len, small_table, q_start=torch.tensor([0, n], dtype=torch.int32, device=device))
+        out, lse_kept = small.attention(q, small_len, small_table, max_kv=n, want_lse=True, **capped)
+        kept = {"kept": out, "kept_tokens": n, "kept_k": k, "small": small, "kept_share": float(torch.exp(lse_kept - lse).mean())}
+    return {**kept, "hidden": hidden, "full": full, "starts": starts, "named": named, "chosen": chosen, "blocks": last + 1,
             **{name: float(torch.stack(x).mean()) for name, x in shares.items()}}
 
 
 if __name__ == "__main__":
-    r = run()
+    r = run(eight_bits="--eight-bits" in sys.argv[1:])
     print(f"{r['blocks']} blocks in the cache, lists of {r['chosen'].shape[2]}: the blocks of the evidence spans hold {r['span_share']:.2f} of the full "
           f"attention's weight, those that each step chooses {r['chosen_share']:.2f} (their part of the cache: {r['chosen'].shape[2] / r['blocks']:.2f})")
+    if "kept" in r:
+        print(f"{r['kept_tokens']} tokens of the spans, read back into a cache of their own, hold {r['kept_share']:.2f} of it")

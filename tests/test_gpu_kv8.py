@@ -571,6 +571,21 @@ def test_used_together_and_captured_in_a_graph(new, eight):
             assert torch.equal(a, b)
 
 
+def test_example_in_eight_bits():
+    """examples/paged_answer.py over a cache of 8 bits: the spans' tokens, read back and kept again, hold what they held (their rows are what 8 bits stand for, so
+    that keeping them again changes nothing), and no list holds more than all of the weight."""
+    from examples import paged_answer
+    r = paged_answer.run(context=3000, chunk=700, answer=3, n_q=8, n_kv=2, n_feat=1024, k=16, top_blocks=12, n_spans=6, eight_bits=True)
+    for name in ("hidden", "full", "kept"):
+        assert torch.isfinite(r[name].float()).all()
+    n, small = r["kept_tokens"], r["small"]
+    assert 0 < n <= 6 * 64 + 1
+    k, _ = small.read(torch.tensor([n], dtype=torch.int32, device="cuda"), torch.arange(small.n_pages, dtype=torch.int32, device="cuda")[None], n,
+                      q_start=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    assert torch.equal(k, r["kept_k"])
+    assert 0.0 < r["span_share"] <= 1.0 + 1e-5 and 12 / r["blocks"] < r["chosen_share"] <= 1.0 + 1e-5 and 0.0 < r["kept_share"] <= 1.0 + 1e-5
+
+
 def test_no_tokens_is_a_no_op():
     pr = paged8.Problem8(17, 128, 64, 8, 2, [0, 0], [10, 0])
     kv_len, table = pr.args()
