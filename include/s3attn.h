@@ -453,7 +453,7 @@ int s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const
  *   scale  [n_pages][n_kv_heads][2][page_size]                 uint8: codes of the keys, then of the values; c stands for 2^(c - 127)
  *   sig    as in s3_kv_cache, or NULL
  * all 256-byte aligned.  Codes go from 1 to 247; others count as the nearer of the two.  What an element stands for is exact in bf16, 2^-126
- * and more of it.  Limits as s3_kv_cache.
+ * and more of it; of 2^128 and more it counts as infinite, or enters a sum as it is.  Limits as s3_kv_cache.
  * Calls take such a cache where their name begins with s3_kv8_; rows that they take and give are bf16.  s3_block_select reads signatures only: give it
  * an s3_kv_cache of S3_BF16 with the same k, v, sig and sizes. */
 typedef struct {

@@ -246,6 +246,28 @@ def test_codes_that_no_append_writes(new):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("new", [2, 90])
+def test_values_beyond_what_fp32_holds(new):
+    """The largest e4m3 value at the largest scale passes 2^128: the rows that see it have an infinite sum, or its share w of it, and it does not reach the others.
+    A weight of the row is off by 2^-8 of itself (bf16), by twice the score's error (64 2^-24 scale sum |q k|, some 2^-13) and by its sum's 2^-24 a token; the
+    result is rounded by 2^-8 of itself, so the share is within 2^-7 + 2^-12 of itself; the other values' part is less than 2^-100 of it."""
+    pr = paged8.Problem8(24, 64, 16, 4, 2, [new], [new + 30])
+    n = new + 30
+    pr.bytes["v"][0][n - 1, 1, 7] = 0x7e
+    pr.codes["v"][0][n - 1, 1] = 247
+    pr.rows_v[0][n - 1, 1] = 0.0
+    o, _ = run(pr, pr.cache())
+    out, _, tol, _ = paged.attend(pr)
+    o = o.cpu().to(torch.float64)
+    others = torch.ones(new, 4, dtype=torch.bool)
+    others[-1, 2:] = False
+    assert torch.all((o - out).abs()[others] <= tol[others])
+    K = pr.rows_k[0][:, 1].to(torch.float64)
+    w = torch.softmax(pr.q[-1, 2:].to(torch.float64) @ K.t() * 64 ** -0.5, 1)[:, n - 1]
+    share, got = w * 448.0 * 2.0 ** 120, o[-1, 2:, 7]
+    assert torch.all((got == float("inf")) | ((got - share).abs() <= (2.0 ** -7 + 2.0 ** -12) * share))
+
+
 def test_two_calls_at_once():
     """On two streams, with a workspace each: as one after the other."""
     pr = paged8.Problem8(23, 128, 64, 8, 2, [1, 1, 90], [3000, 70, 500])
