@@ -7,8 +7,8 @@
 // 32768 with d_head 64: 42 / 27, of eight at 8000 with 256: 258 / 208, in fp32: 355 / 217 (32 tokens: 579 / 375); tiles of 16
 // queries over 64 listed blocks of 512: 343 / 240, d_head 64: 276 / 154.  But bf16 with d_head 128, eight sequences: 66 / 73, where the tiled
 // kernel's rate is best.
-constexpr int s3_few_rows(bool bf16, int d_head, bool list) {
-    return !bf16 ? (d_head == 128 ? 128 : 64) : list || d_head != 128 ? 64 : 32;
+constexpr int s3_few_rows(bool bf16, int d_head, bool list, bool eight) {
+    return !bf16 ? (d_head == 128 ? 128 : 64) : list || eight || d_head != 128 ? 64 : 32;
 }
 
 // Over an 8-bit cache, and with capped scores over one of bf16, 16 rows are a tile of their own, and whether one workgroup takes all tokens of such a tile and head, which saves the joining launch, or the

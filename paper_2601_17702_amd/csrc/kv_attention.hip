@@ -29,7 +29,11 @@ struct Plan {
     size_t bytes() const { return few_ws + many_ws; }
     Plan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b, int window) {
         G = n_q / c->n_kv_heads;
-        limit = s3_few_rows(c->dtype != S3_FP32, c->d_head, q_block != 0);
+        limit = s3_few_rows(c->dtype != S3_FP32, c->d_head, q_block != 0, c->dtype == kS3E4m3);
+        // Over 8 bits rows 33 to 64 are the streaming kernel's where there is much to stream, whose bytes then bound it.  us there / in the tiled kernel, 12 tokens of 32 heads
+        // over 8: d_head 128, 4 sequences of 8000 37 / 33, of 16000 49 / 53, 16 of 8000 88 / 92, of 32000 273 / 355; 64, 4 of 4000 23 / 17, of 8000 29 / 29, 16 of 16000
+        // 105 / 165; 256, 16 of 4000 120 / 102, of 8000 188 / 186, of 32000 513 / 719.
+        if (c->dtype == kS3E4m3 && !q_block) limit = (int64_t)min(b->n_seq, b->n_tokens) * c->n_kv_heads * b->max_kv >= 4096 * c->d_head ? 64 : 32;
         qb = min(q_block, max(b->n_tokens, 1));
         const int most_new = min(max(b->max_new, 1), max(b->n_tokens, 1));
         const int64_t most = (int64_t)(q_block ? min(qb, most_new) : most_new) * G;

@@ -22,6 +22,8 @@ SHAPES = [   # d, P, hq, hkv, new, kv
     (64, 64, 32, 1, [3, 1], [900, 40]),                       # 96 rows of three tokens
     (256, 32, 3, 1, [1, 1], [3001, 33]),                      # an odd number of rows, in parts
     (128, 16, 4, 1, [300], [301]),
+    (128, 32, 8, 2, [12, 1, 16], [700, 40, 16]),              # 48 and 64 rows
+    (64, 16, 4, 4, [50, 40], [400, 50]),
 ]
 
 
@@ -38,6 +40,7 @@ def test_attention(d, P, hq, hkv, new, kv):
     o, lse = run(pr, c, max_new=max(new), max_kv=max(kv))
     paged.check(pr, o, lse, want)
     assert torch.equal(o, run(pr, c, max_new=max(new), max_kv=max(kv))[0])       # the same bits every time
+    paged.check(pr, *run(pr, c, max_new=max(new), max_kv=1 << 20), want)         # a bound that makes more rows the streaming kernel's
 
 
 @pytest.mark.parametrize("d,P,hq,hkv,new,kv,window", [(128, 64, 8, 2, [1, 1], [500, 3], 100), (64, 16, 8, 2, [90], [400], 1),
