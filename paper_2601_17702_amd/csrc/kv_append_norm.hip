@@ -6,7 +6,9 @@
 // A power of two as a scale costs no precision (e4m3 values have the same 4 bits in every octave of 17) and makes both scalings exact.
 //
 // What bounds it: memory.  A row of d channels lies in d / 16 lanes, 16 channels each: where pairs are (i, i + rot / 2) eight of one half and
-// their eight partners, so a rotation needs no other lane's channels, and a norm's sum is exchanged between neighbours of a row of 16 lanes only.
+// their eight partners, so a rotation needs no other lane's channels, and a norm's sum is exchanged between neighbours of a row of 16 lanes only.  Two rows' loads are under way
+// in a thread before the first is worked on.  Eight chunks of 2048 tokens into 8 bits, 32 query heads over 8 of 128 (387 MB): 82 to 85 us, 4.6 TB/s; 116 with 8 channels a
+// lane and no loads ahead, 134 with 16 and none, 86 with four rows'.  64 single tokens: 6.7 us, a chain of loads.
 #include "kv_cache.h"
 
 namespace {
