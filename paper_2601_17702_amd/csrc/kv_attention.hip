@@ -33,7 +33,7 @@ struct Plan {
         // Over 8 bits rows 33 to 64 are the streaming kernel's where there is much to stream, whose bytes then bound it.  us there / in the tiled kernel, 12 tokens of 32 heads
         // over 8: d_head 128, 4 sequences of 8000 37 / 33, of 16000 49 / 53, 16 of 8000 88 / 92, of 32000 273 / 355; 64, 4 of 4000 23 / 17, of 8000 29 / 29, 16 of 16000
         // 105 / 165; 256, 16 of 4000 120 / 102, of 8000 188 / 186, of 32000 513 / 719.
-        if (c->dtype == kS3E4m3 && !q_block) limit = (int64_t)min(b->n_seq, b->n_tokens) * c->n_kv_heads * b->max_kv >= 4096 * c->d_head ? 64 : 32;
+        if (c->dtype == kS3E4m3 && !q_block) limit = (double)min(b->n_seq, b->n_tokens) * c->n_kv_heads * b->max_kv >= 4096.0 * c->d_head ? 64 : 32;
         qb = min(q_block, max(b->n_tokens, 1));
         const int most_new = min(max(b->max_new, 1), max(b->n_tokens, 1));
         const int64_t most = (int64_t)(q_block ? min(qb, most_new) : most_new) * G;
