@@ -510,6 +510,8 @@ class KVCache:
     a batch of single tokens is planned as if chunks were among them, with their launch and workspace).  Arrays of rows are [n_tokens, heads, d_head],
     the last axis contiguous, the others of any stride that is a multiple of 16 bytes."""
 
+    _eight = False            # whether the cache is one of 8 bits
+
     def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, dtype=None, signatures: bool = False,
                  device="cuda", k=None, v=None, sig=None):
         import torch
@@ -584,7 +586,7 @@ class KVCache:
         if q is not None:
             qp, qt, qh, n_q = self._rows(q, T)
             if q_out is None:
-                q_out = q.new_empty(q.shape)
+                q_out = _torch().empty_like(q, memory_format=_torch().contiguous_format)
             else:
                 assert q_out.shape == q.shape and q_out.dtype is q.dtype and q_out.is_contiguous() and q_out.is_cuda
             op = q_out.data_ptr()
@@ -593,14 +595,14 @@ class KVCache:
             assert q_norm is None or q is not None
             (qw, qs), (kw, ks) = self._weights(q_norm, n_q), self._weights(k_norm, heads)
             norm = _KV_NORM.pack(qw, kw, qs, ks, eps)
-        rc = self._append((self._c, b, kp, kt, kh, vp, vt, vh, rp, n_pos, rot, interleaved, _ptr(positions), qp, n_q, qt, qh, op), norm)
+        args = self._c, b, kp, kt, kh, vp, vt, vh, rp, n_pos, rot, interleaved, _ptr(positions), qp, n_q, qt, qh, op
+        if self._eight:
+            rc = _lib.s3_kv8_append(*args, norm, _stream())
+        else:
+            rc = _lib.s3_kv_append(*args, _stream()) if norm is None else _lib.s3_kv_append_norm(*args, norm, _stream())
         if rc:
             _check(rc)
         return q_out
-
-    @staticmethod
-    def _append(args, norm):
-        return _lib.s3_kv_append(*args, _stream()) if norm is None else _lib.s3_kv_append_norm(*args, norm, _stream())
 
     def read(self, kv_len, block_table, n_rows: int, q_start=None, positions=None, k_out=None, v_out=None):
         """s3_kv_read: tokens back as rows.  Rows q_start[s] .. q_start[s + 1] - 1 (None: row s) are those of sequence s at `positions`
@@ -613,15 +615,11 @@ class KVCache:
         for x in (k_out, v_out):
             assert x is None or (x.is_cuda and x.is_contiguous() and x.dtype is self.dtype and x.shape == shape)
         k = self.k.new_empty(shape, dtype=self.dtype) if k_out is None else k_out
-        v = self.k.new_empty(shape, dtype=self.dtype) if v_out is None else v_out
-        rc = self._read(self._c, b, _ptr(positions), k.data_ptr(), v.data_ptr(), _stream())
+        v = torch.empty_like(k) if v_out is None else v_out
+        rc = (_lib.s3_kv8_read if self._eight else _lib.s3_kv_read)(self._c, b, _ptr(positions), k.data_ptr(), v.data_ptr(), _stream())
         if rc:
             _check(rc)
         return k, v
-
-    @staticmethod
-    def _read(*args):
-        return _lib.s3_kv_read(*args)
 
     @staticmethod
     def _scratch(q, need, ws):
@@ -631,28 +629,13 @@ class KVCache:
         return ws
 
     def _out(self, q, out, want_lse, need, ws):
+        torch = _torch()
         if out is None:
-            out = q.new_empty(q.shape)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
             assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.is_cuda
-        lse = q.new_empty(q.shape[:2], dtype=_torch().float32) if want_lse else None
+        lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
         return out, lse, self._scratch(q, need, ws)
-
-    def _attend(self, head, scale, softcap, window, tail):
-        if softcap:
-            return _lib.s3_paged_attention_capped(*head, scale, softcap, window, *tail)
-        return _lib.s3_paged_attention(*head, scale, window, *tail)
-
-    def _attend_blocks(self, head, scale, softcap, tail):
-        if softcap:
-            return _lib.s3_block_attention_capped(*head, scale, softcap, *tail)
-        return _lib.s3_block_attention(*head, scale, *tail)
-
-    def _attend_workspace(self, *args):
-        return _lib.s3_paged_attention_workspace(*args)
-
-    def _attend_blocks_workspace(self, *args):
-        return _lib.s3_block_attention_workspace(*args)
 
     def attention(self, q, kv_len, block_table, q_start=None, scale=None, window: int = 0, max_new=None, max_kv=None, out=None,
                   want_lse: bool = False, ws=None, softcap: float = 0.0):
@@ -661,10 +644,18 @@ class KVCache:
         T, n_q, _ = q.shape
         b = self._batch(T, kv_len, block_table, q_start, max_new, max_kv)
         qp, qt, qh, _ = self._rows(q, T)
-        need = self._attend_workspace(self._c, b, n_q)
+        c, L = self._c, _lib
+        need = (L.s3_kv8_attention_workspace if self._eight else L.s3_paged_attention_workspace)(c, b, n_q)
         out, lse, ws = self._out(q, out, want_lse, need, ws)
-        rc = self._attend((self._c, b, qp, n_q, qt, qh), self.scale if scale is None else scale, softcap, window,
-                          (out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+        if scale is None:
+            scale = self.scale
+        op, lp, wp, size = out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel()
+        if self._eight:
+            rc = L.s3_kv8_attention(c, b, qp, n_q, qt, qh, scale, softcap, window, op, lp, wp, size, _stream())
+        elif softcap:
+            rc = L.s3_paged_attention_capped(c, b, qp, n_q, qt, qh, scale, softcap, window, op, lp, wp, size, _stream())
+        else:
+            rc = L.s3_paged_attention(c, b, qp, n_q, qt, qh, scale, window, op, lp, wp, size, _stream())
         if rc:
             _check(rc)
         return out, lse
@@ -696,10 +687,18 @@ class KVCache:
         tiles, heads, top_b = sel.shape
         assert sel.is_cuda and sel.is_contiguous() and sel.dtype is kv_len.dtype and heads == self.n_kv_heads
         assert tiles >= _lib.s3_block_tiles(b, q_block)
-        need = self._attend_blocks_workspace(self._c, b, n_q, q_block, top_b)
+        c, L = self._c, _lib
+        need = (L.s3_kv8_block_attention_workspace if self._eight else L.s3_block_attention_workspace)(c, b, n_q, q_block, top_b)
         out, lse, ws = self._out(q, out, want_lse, need, ws)
-        rc = self._attend_blocks((self._c, b, qp, n_q, qt, qh, sel.data_ptr(), q_block, top_b), self.scale if scale is None else scale, softcap,
-                                 (out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+        if scale is None:
+            scale = self.scale
+        sp, op, lp, wp, size = sel.data_ptr(), out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel()
+        if self._eight:
+            rc = L.s3_kv8_block_attention(c, b, qp, n_q, qt, qh, sp, q_block, top_b, scale, softcap, op, lp, wp, size, _stream())
+        elif softcap:
+            rc = L.s3_block_attention_capped(c, b, qp, n_q, qt, qh, sp, q_block, top_b, scale, softcap, op, lp, wp, size, _stream())
+        else:
+            rc = L.s3_block_attention(c, b, qp, n_q, qt, qh, sp, q_block, top_b, scale, op, lp, wp, size, _stream())
         if rc:
             _check(rc)
         return out, lse
@@ -709,6 +708,8 @@ class KVCache8(KVCache):
     """The same in 8 bits (s3_kv8_cache): half of a bf16 cache's memory, and of its traffic.  k [n_pages, n_kv_heads, d_head / 16, page_size, 16] and
     v [n_pages, n_kv_heads, page_size / 16, d_head, 16] in float8_e4m3fn, scale [n_pages, n_kv_heads, 2, page_size] uint8: element times
     2^(code - 127) is what it stands for.  Every call of KVCache is here, with the same arguments; rows are bfloat16."""
+
+    _eight = True
 
     def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, signatures: bool = False, device="cuda", k=None, v=None,
                  scale=None, sig=None):
@@ -730,23 +731,3 @@ class KVCache8(KVCache):
         sizes = (n_pages, page_size, n_kv_heads, d_head)
         self._c = _KV8_CACHE.pack(_ptr(self.k), _ptr(self.v), _ptr(self.codes), _ptr(self.sig) or 0, *sizes)
         self._c16 = _KV_CACHE.pack(_ptr(self.k), _ptr(self.v), _ptr(self.sig) or 0, S3_BF16, *sizes)      # for the choice, which reads sig only
-
-    @staticmethod
-    def _append(args, norm):
-        return _lib.s3_kv8_append(*args, norm, _stream())
-
-    @staticmethod
-    def _read(*args):
-        return _lib.s3_kv8_read(*args)
-
-    def _attend(self, head, scale, softcap, window, tail):
-        return _lib.s3_kv8_attention(*head, scale, softcap, window, *tail)
-
-    def _attend_blocks(self, head, scale, softcap, tail):
-        return _lib.s3_kv8_block_attention(*head, scale, softcap, *tail)
-
-    def _attend_workspace(self, *args):
-        return _lib.s3_kv8_attention_workspace(*args)
-
-    def _attend_blocks_workspace(self, *args):
-        return _lib.s3_kv8_block_attention_workspace(*args)
