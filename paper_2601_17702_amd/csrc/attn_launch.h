@@ -36,8 +36,17 @@ size_t s3_attn_tile_workspace(const s3_kv_cache* c, int64_t units, int n_split);
 struct TileArgs {
     float* slots;             // partial sums where n_split > 1
     int n_split, tiles;       // row tiles that there can be
+    bool small;               // of 128 rows, where a call's other tiles would have 256
 };
-int s3_attn_tile(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int n_split, void* ws, hipStream_t st);
+int s3_attn_tile(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int n_split, bool small, void* ws, hipStream_t st);
+// Whether an uncut call of the builds for 8 bits and for caps takes tiles of 128 rows: where those of 256 would leave half of the 256 compute
+// units idle. Dim 128, 8 heads with 4 query heads each, one sequence, tiles of 256 rows against tiles of 128, in us: 64 tokens of e4m3 11
+// against 9, 256 17 against 15, 512 24 against 22, 1024 (128 units) 39 against 38; with bf16 and a cap 12 against 9, 19 against 16, 28
+// against 24, 47 against 41. At 160 units and more it turns: four sequences of 300 tokens 18 against 23, of 2048 (256 units) 71 against 79.
+constexpr bool s3_has_small_tiles(bool eight, bool bf16, int d_head, bool cap) { return (eight || (bf16 && cap)) && d_head <= 128; }
+constexpr bool s3_small_tiles(bool eight, bool bf16, int d_head, bool cap, int64_t units, int n_split) {
+    return s3_has_small_tiles(eight, bf16, d_head, cap) && n_split == 1 && units <= 128;
+}
 int s3_attn_tile_cap(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);
 int s3_attn_tile_8(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);
 int s3_attn_tile_8_cap(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);

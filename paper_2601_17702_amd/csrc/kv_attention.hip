@@ -24,7 +24,7 @@ int check_ws(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
 struct Plan {
     int G, R, qb, per_q, n_split, limit;
     bool few, many;
-    int64_t few_tiles, many_tiles, few_tokens;
+    int64_t few_tiles, many_tiles, few_tokens, most, all, longs, q_tiles;
     size_t few_ws, many_ws;
     size_t bytes() const { return few_ws + many_ws; }
     Plan(const s3_kv_cache* c, const s3_kv_batch* b, int n_q, int q_block, int top_b, int window) {
@@ -36,7 +36,7 @@ struct Plan {
         if (c->dtype == kS3E4m3 && !q_block) limit = (double)min(b->n_seq, b->n_tokens) * c->n_kv_heads * b->max_kv >= 4096.0 * c->d_head ? 64 : 32;
         qb = min(q_block, max(b->n_tokens, 1));
         const int most_new = min(max(b->max_new, 1), max(b->n_tokens, 1));
-        const int64_t most = (int64_t)(q_block ? min(qb, most_new) : most_new) * G;
+        most = (int64_t)(q_block ? min(qb, most_new) : most_new) * G;
         many = most > limit;
         // Beside chunks up to 32 rows: more of them fill what the chunk leaves idle or not, by lengths that the host does not know.  us with 32 / with
         // s3_few_rows, 8 sequences of 16 tokens beside 512 at 2048: at 1000 tokens with d_head 256 139 / 200, in fp32 with 128 296 / 358, with 256 726 / 872; at 8000
@@ -47,12 +47,11 @@ struct Plan {
         few = !many || (!q_block && !all_long);
         R = (int)min(most, (int64_t)limit);                    // a sequence's, or a tile of listed blocks', are one row tile
         const int rows = s3_attn_tile_rows(c);
-        per_q = (int)((most + rows - 1) / rows);
-        few_tiles = q_block ? s3_block_tiles(b, q_block) : min(b->n_seq, b->n_tokens);
-        // row tiles that there can be: beside the streaming kernel only sequences of more than `limit` rows have any, and each ends in one
-        // that is not full; none has more than max_new tokens
-        const int64_t all = (int64_t)b->n_tokens * G, longs = min((int64_t)min(b->n_seq, b->n_tokens), few ? all / (limit + 1) : all);
-        many_tiles = !many ? 0 : q_block ? s3_block_tiles(b, q_block) * per_q : min((all + longs * (rows - 1)) / rows, longs * ((most + rows - 1) / rows));
+        q_tiles = q_block ? s3_block_tiles(b, q_block) : 0;
+        few_tiles = q_block ? q_tiles : min(b->n_seq, b->n_tokens);
+        all = (int64_t)b->n_tokens * G;
+        longs = min((int64_t)min(b->n_seq, b->n_tokens), few ? all / (limit + 1) : all);
+        cut(rows);
         const int64_t units = many_tiles * c->n_kv_heads;
         const int64_t tokens = few_tokens = q_block ? (int64_t)top_b * c->page_size : b->max_kv;
         const bool ragged = !q_block && b->n_seq > 1;
@@ -62,9 +61,17 @@ struct Plan {
         if (window && !q_block) few_tokens = min(tokens, (int64_t)window + R / G + 32);
         if (many && window) n_split = min(n_split, s3_attn_tile_split(c, units, min(tokens, (int64_t)window + rows / G), ragged));
     }
+    // Row tiles that there can be: beside the streaming kernel only sequences of more than `limit` rows have any, and each ends in one
+    // that is not full; none has more than max_new tokens.
+    void cut(int rows) {
+        per_q = (int)((most + rows - 1) / rows);
+        many_tiles = !many ? 0 : q_tiles ? q_tiles * per_q : min((all + longs * (rows - 1)) / rows, longs * ((most + rows - 1) / rows));
+    }
 };
 
-int run(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b, AttnArgs p, const Plan& plan, void* ws, hipStream_t st) {
+int run(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b, AttnArgs p, Plan plan, void* ws, hipStream_t st) {
+    const bool small = plan.many && s3_small_tiles(c->dtype == kS3E4m3, c->dtype != S3_FP32, c->d_head, p.cap != 0.0f, plan.many_tiles * c->n_kv_heads, plan.n_split);
+    if (small) plan.cut(128);
     p.few = plan.few ? plan.limit : 0;
     p.qb = plan.qb;
     p.per_q = plan.per_q;
@@ -73,7 +80,7 @@ int run(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b, AttnArgs p, 
         return s3_fail(S3_EINVAL, "%s: %lld row tiles and %d heads are too many for one call", fn, (long long)max(plan.few_tiles, plan.many_tiles), c->n_kv_heads);
     if (plan.few)
         if (int rc = s3_attn_stream(c, p, plan.few_tiles, plan.R, plan.few_tokens, ws, st)) return rc;
-    return plan.many ? s3_attn_tile(c, p, plan.many_tiles, plan.n_split, (char*)ws + plan.few_ws, st) : S3_OK;
+    return plan.many ? s3_attn_tile(c, p, plan.many_tiles, plan.n_split, small, (char*)ws + plan.few_ws, st) : S3_OK;
 }
 
 bool shapes_ok(const s3_kv_cache* c, const s3_kv_batch* b, int n_q) {

@@ -169,6 +169,16 @@ def test_tiles_that_one_workgroup_has_and_that_are_cut(dtype, cap, n_seq, hkv, l
     paged.check(pr, o, lse, paged8.attend(pr, cap, window=window) if cap else paged.attend(pr, window=window))
 
 
+@pytest.mark.parametrize("dtype,d,cap", [("e4m3", 128, 0.0), ("e4m3", 64, 5.0), ("bf16", 128, 5.0), ("bf16", 64, 5.0)])
+@pytest.mark.parametrize("hkv,G,new", [(16, 8, [256]), (16, 8, [230, 20, 6]), (16, 8, [257]), (16, 4, [200, 0, 150, 60]), (1, 1, [65]), (2, 32, [3])])
+def test_tiles_of_few_and_of_many_rows(dtype, d, cap, hkv, G, new):
+    """Both sides of the rule that halves the row tiles of calls with few of them: 128 tiles of all heads, 144, and next to none."""
+    pr = paged8.problem(dtype, d + len(new), d, 32, hkv * G, hkv, new, [n + 3 if n else 0 for n in new])
+    kv_len, table = pr.args()
+    o, lse = pr.cache().attention(pr.q.cuda(), kv_len, table, q_start=pr.q_start.cuda(), max_new=max(new), max_kv=max(new) + 3, softcap=cap, want_lse=True)
+    paged.check(pr, o, lse, paged8.attend(pr, cap) if cap else paged.attend(pr))
+
+
 @pytest.mark.parametrize("listed", [False, True])
 @pytest.mark.parametrize("dtype,new,G,n_seq,cap", [("e4m3", 1, 4, 1200, 0.0), ("e4m3", 1, 4, 1, 0.0), ("e4m3", 8, 4, 200, 0.0), ("e4m3", 64, 4, 100, 0.0), ("e4m3", 70, 4, 1, 5.0),
                                                    ("bf16", 1, 4, 1200, 5.0), ("bf16", 64, 4, 3, 5.0)])
