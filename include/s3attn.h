@@ -491,7 +491,7 @@ int s3_kv8_append(const s3_kv8_cache* cache, const s3_kv_batch* batch, const voi
 
 /* s3_paged_attention and s3_block_attention with capped scores: softmax over softcap * tanh(scale q . k / softcap), lse of these.
  * Masks hide a token from the softmax, whatever the cap.  0 < softcap <= 1e30, scale / softcap from 1e-30 to 1e30; workspaces as theirs.  A score is within 2^-20 of its magnitude, with rows
- * of bf16 and softcap <= 2048 within 2^-22 of softcap more. */
+ * of bf16 and softcap <= 2048 within 2^-22 of softcap more; lse is off by no more than its scores are, and what its sum and logarithm round without a cap, too. */
 int s3_paged_attention_capped(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
                               int64_t q_tok_stride, int64_t q_head_stride, float scale, float softcap, int window, void* out,
                               float* lse, void* ws, size_t ws_bytes, void* stream);

@@ -39,7 +39,7 @@ struct AttnArgs {
     int n_kv, G, n_q, window;
     int qb, top, per_q, lists;// lists: tokens a tile, entries, row tiles a tile of queries (tiled kernel), how many lists there are
     float sl;                 // scale * log2(e), or what capped scores are to be multiplied by
-    float cap, to_cap, cap_lse;      // with a cap (0: none): cap * log2(e), scale / cap, and what lse is less by where the capped scores come shifted
+    float cap, to_cap, cap_lse;      // with a cap (0: none): cap * log2(e), scale / cap, and how far up the capped scores come shifted (log2 units)
     int few;                  // sequences of at most this many rows are the streaming kernel's
 };
 
@@ -247,8 +247,9 @@ struct AttnState {
 
 // Capped scores of this lane's raw ones x: c tanh(z), z = x u, in log2 units.
 //
-// NEAR: c tanh(z) = 2 c r - c with r = 1 / (1 + exp(-2 z)); r takes the score's place, 2 c that of the scale, and softmax does not see the shift, which lse takes off
-// at the end: a multiplication, an addition and two quarter-rate instructions a score more than without a cap.  r is off by 2^-23 or so, the score by 2^-22 c: for
+// NEAR: c tanh(z) = 2 c r - c with r = 1 / (1 + exp(-2 z)); r takes the score's place, 2 c that of the scale, and softmax does not see the shift: a multiplication,
+// an addition and two quarter-rate instructions a score more than without a cap.  lse takes it off the maximum, an exact difference from r = 1/4 on, before the sum's logarithm is
+// added: behind that it is rounded to the cap's places, 2e-4 off for 5e-5 at a cap of 2048.  r is off by 2^-23 or so, the score by 2^-22 c: for
 // rows of bf16, whose weights are rounded to 2^-8 of themselves, up to caps of 2048 (5e-4 there).
 // Otherwise, for scores as exact as fp32 ones whatever the cap: below |z| = 0.35 by tanh's series (its next term, 1382 z^11 / 155925, is 2^-22 of z there), above as
 // 1 - 2 / (1 + exp(2 z)).  Where all of a wavefront's are small, as a cap well above the scores leaves them, only the series runs.

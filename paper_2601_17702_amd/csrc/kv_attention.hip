@@ -120,7 +120,7 @@ int attend(const Call& x, int window, const int32_t* sel, int q_block, int top_b
     const AttnArgs p{s3_kv_batch_args(&c, x.b), (const char*)x.q, (char*)x.out, x.lse, (const char*)c.k, (const char*)c.v, x.scale8, sel, x.q_ts * es,
                      x.q_hs * es, c.n_kv_heads, plan.G, x.n_q, window, 0, top_b, 1, q_block ? (int)s3_block_tiles(x.b, q_block) : 0,
                      near ? 2.0f * x.softcap * log2e : cap ? 1.0f : x.scale * log2e, cap ? x.softcap * log2e : 0.0f, cap ? x.scale / x.softcap : 0.0f,
-                     near ? x.softcap : 0.0f, 0};
+                     near ? x.softcap * log2e : 0.0f, 0};
     return run(x.fn, &c, x.b, p, plan, x.ws, (hipStream_t)x.stream);
 }
 int check_window(const char* fn, int window) { return window < 0 ? s3_fail(S3_EINVAL, "%s: window %d", fn, window) : S3_OK; }
