@@ -125,17 +125,17 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs p) {
             char* dst = p.k + (((int64_t)(t0 + r) * p.n_kv + h) * D + g * E) * (int)sizeof(T);
             if constexpr (EIGHT) {
                 const float f = page >= 0 ? kv_scale(p.scale[unit * (2 * P) + slots[r]]) : 0.0f;
-                typedef __attribute__((ext_vector_type(16))) __bf16 row16;
-                row16 y;
+                kv_bf16x8 y[2];                         // k_out is aligned to 16 bytes, no more
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const kv_f32x2 a = kv_of8<false>(x[w]), b = kv_of8<true>(x[w]);
-                    y[4 * w] = (__bf16)(a[0] * f);
-                    y[4 * w + 1] = (__bf16)(a[1] * f);
-                    y[4 * w + 2] = (__bf16)(b[0] * f);
-                    y[4 * w + 3] = (__bf16)(b[1] * f);
+                    y[w / 2][w % 2 * 4] = (__bf16)(a[0] * f);
+                    y[w / 2][w % 2 * 4 + 1] = (__bf16)(a[1] * f);
+                    y[w / 2][w % 2 * 4 + 2] = (__bf16)(b[0] * f);
+                    y[w / 2][w % 2 * 4 + 3] = (__bf16)(b[1] * f);
                 }
-                *(row16*)dst = y;
+                *(kv_bf16x8*)dst = y[0];
+                *(kv_bf16x8*)(dst + 16) = y[1];
             } else {
                 *(kv_u32x4*)dst = x;
             }

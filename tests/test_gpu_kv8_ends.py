@@ -1,4 +1,4 @@
-"""GPU checks at the ends of what the capped and 8-bit calls take: log-sum-exps under large caps."""
+"""GPU checks at the ends of what the capped and 8-bit calls take: log-sum-exps under large caps, outputs at 16 modulo 32 bytes."""
 import pytest
 import torch
 
@@ -33,3 +33,22 @@ def test_lse_of_scores_of_zero(dtype, d, hq, hkv, new, kv, cap):
         _, lse = run(pr, pr.cache(), softcap=cap, **bounds)
         want = torch.log(sees)[:, None]
         assert torch.all((lse.cpu().to(torch.float64) - want).abs() <= 2.0 ** -22 * want)
+
+
+@pytest.mark.parametrize("dtype", ["e4m3", "bf16", "fp32"])
+@pytest.mark.parametrize("d,new", [(64, 40), (128, 3), (256, 33)])
+def test_read_into_outputs_aligned_to_16_bytes(dtype, d, new):
+    """k_out and v_out that begin 16 bytes into their storage, rows in order and far apart: the same bits, and nothing beside them."""
+    pr = paged8.problem(dtype, 31 + d, d, 32, 2, 2, [new], [new + 60])
+    c = pr.cache()
+    kv_len, table = pr.args()
+    e = 16 // pr.dtype.itemsize
+    for positions in (None, torch.arange(new, dtype=torch.int32, device="cuda") * 37 % (new + 60)):
+        same = dict(q_start=pr.q_start.cuda(), positions=positions)
+        want = c.read(kv_len, table, new, **same)
+        rooms = [torch.full((new * 2 * d + 2 * e,), 3.0, dtype=pr.dtype, device="cuda") for _ in "kv"]
+        outs = [x[e:-e].view(new, 2, d) for x in rooms]
+        assert all(x.data_ptr() % 32 == 16 for x in outs)
+        c.read(kv_len, table, new, k_out=outs[0], v_out=outs[1], **same)
+        for room, out, w in zip(rooms, outs, want):
+            assert torch.equal(out, w) and torch.all(room[:e] == 3.0) and torch.all(room[-e:] == 3.0)
