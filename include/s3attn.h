@@ -407,7 +407,9 @@ int s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const void*
  * Softmax statistics and sums in fp32; with bf16 the weights are rounded to bf16 for the second product, their sum is not: outputs are
  * within 2^-8 of the weighted sum of magnitudes, and once more 2^-8 of themselves by their own rounding.
  *   q    [n_tokens][n_q_heads][d_head], strides as in s3_kv_append;  out [n_tokens][n_q_heads][d_head] contiguous, dtype
- *   ws   s3_paged_attention_workspace(...) bytes, 256-byte aligned, contents meaningless between calls
+ *   ws   s3_paged_attention_workspace(...) bytes, 256-byte aligned, contents meaningless between calls.  The size is this call's: a smaller batch, which is cut into
+ *        more parts, may take more.  Where max_new * G <= 32 (lists: min(max_new, q_block) * G) no batch takes more than one of a single sequence with n_tokens = max_new
+ *        and the same max_kv (top_b), so that a buffer of that size is enough for all of them; with longer chunks ask before every call
  * Limits: 1 <= G <= 32; scale > 0; window >= 0.  n_kv_heads times n_seq below 2^22, and times the chunks' tiles of 128 rows (n_tokens * G / 128,
  * one more for every sequence of more than 32 rows). */
 size_t s3_paged_attention_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads);
@@ -500,7 +502,8 @@ int s3_block_attention_capped(const s3_kv_cache* cache, const s3_kv_batch* batch
                               float scale, float softcap, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* s3_paged_attention and s3_block_attention over an 8-bit cache; q and out are bf16.  softcap as above, or 0: none.  Keys and values enter as what
- * they stand for, exactly; the weights are rounded to bf16, as over a bf16 cache. */
+ * they stand for, exactly; the weights are rounded to bf16, as over a bf16 cache.  Many short sequences need no workspace where few do (0 bytes, ws may be NULL): what
+ * stands at s3_paged_attention of a buffer for all batches holds here, too. */
 size_t s3_kv8_attention_workspace(const s3_kv8_cache* cache, const s3_kv_batch* batch, int n_q_heads);
 int s3_kv8_attention(const s3_kv8_cache* cache, const s3_kv_batch* batch, const void* q, int n_q_heads,
                      int64_t q_tok_stride, int64_t q_head_stride, float scale, float softcap, int window, void* out, float* lse,

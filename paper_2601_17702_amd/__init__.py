@@ -508,7 +508,8 @@ class KVCache:
     [n_seq, max_pages] int32, page numbers; q_start [n_seq + 1] int32, rows of the new tokens (None: one per sequence); max_new and
     max_kv, bounds of the new tokens and of kv_len that the host knows (they share out the work; give max_new with q_start, without it
     a batch of single tokens is planned as if chunks were among them, with their launch and workspace).  Arrays of rows are [n_tokens, heads, d_head],
-    the last axis contiguous, the others of any stride that is a multiple of 16 bytes."""
+    the last axis contiguous, the others of any stride that is a multiple of 16 bytes.  ws: scratch of a call, uint8 of the size that the library's
+    ..._workspace names for this very call (a smaller batch may take more: s3_paged_attention in the header says which size is enough for all); None: allocated here."""
 
     _eight = False            # whether the cache is one of 8 bits
 
