@@ -5,6 +5,8 @@
 // are per lane, and its 16 weights are, as they lie, the second product's operand.  For that the tokens are dealt to the first product's
 // rows in an order of their own (kv_token): register i of half h is token 2 E (i / E) + E h + i % E of the 32.
 #pragma once
+#include <type_traits>
+
 #include "kv_cache.h"
 
 template <int D, typename T> constexpr int kQSteps = D * (int)sizeof(T) / 32;       // 16-byte pieces of a row per lane
@@ -33,15 +35,21 @@ struct AttnArgs {
     float* lse;
     const char* k;
     const char* v;
-    const uint8_t* scale;     // an 8-bit cache's
     const int32_t* sel;       // block lists, or null: all blocks
     int64_t q_ts, q_hs;       // bytes
     int n_kv, G, n_q, window;
     int qb, top, per_q, lists;// lists: tokens a tile, entries, row tiles a tile of queries (tiled kernel), how many lists there are
     float sl;                 // scale * log2(e), or what capped scores are to be multiplied by
-    float cap, to_cap, cap_lse;      // with a cap (0: none): cap * log2(e), scale / cap, and how far up the capped scores come shifted (log2 units)
     int few;                  // sequences of at most this many rows are the streaming kernel's
 };
+// What 8-bit caches and caps need beside.  The other builds are launched without it: every argument is read from memory when a workgroup begins, and with these 0.1 to 0.7 us
+// of a tiled call's two launches were lost (16 tokens at 20000, 28 heads over 4: 28.1 -> 28.8; 333 at 333 in fp32 with 256 channels: 37.6 -> 38.3).
+struct AttnMore : AttnArgs {
+    const uint8_t* scale;     // an 8-bit cache's
+    float cap, to_cap, cap_lse;      // with a cap (0: none): cap * log2(e), scale / cap, and how far up the capped scores come shifted (log2 units)
+};
+template <typename S, bool CAP> using kAttnArgs = std::conditional_t<KvStore<S>::EIGHT || CAP, AttnMore, AttnArgs>;
+template <bool CAP> using kJoinArgs = std::conditional_t<CAP, AttnMore, AttnArgs>;
 
 // Largest over the two lanes that share a row; their sum.  The swap hands every lane both halves' values.
 __device__ __forceinline__ float kv_pair_max(float x) {
@@ -256,16 +264,21 @@ struct AttnState {
 // us with the second / with the first, chunks of 333, 826 and 2048 tokens that see 4096 each, 32 heads over 8, bf16: 484 / 342.
 constexpr float kS3NearCap = 2048.0f;
 template <typename V, int N>
-__device__ __forceinline__ void kv_cap_near(V (&s)[N], const AttnArgs& p) {
+__device__ __forceinline__ void kv_cap_near(V (&s)[N], const AttnMore& p) {
     const float k = -2.8853900817779268f * p.to_cap;
 #pragma unroll
     for (int x = 0; x < N; ++x)
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(V) / 4); ++i) s[x][i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[x][i] * k));
 }
-__device__ __forceinline__ bool kv_near(const AttnArgs& p) { return p.cap_lse != 0.0f; }
+__device__ __forceinline__ bool kv_near(const AttnMore& p) { return p.cap_lse != 0.0f; }
+template <bool CAP, typename A>
+__device__ __forceinline__ float kv_shift(const A& p) {
+    if constexpr (CAP) return p.cap_lse;
+    else return 0.0f;
+}
 template <typename V, int N>
-__device__ __forceinline__ void kv_cap_far(V (&s)[N], const AttnArgs& p) {
+__device__ __forceinline__ void kv_cap_far(V (&s)[N], const AttnMore& p) {
     const float u = p.to_cap, c = p.cap;
     float most = 0.0f;
 #pragma unroll
@@ -290,7 +303,7 @@ __device__ __forceinline__ void kv_cap_far(V (&s)[N], const AttnArgs& p) {
 }
 
 template <bool BF16, typename V, int N>
-__device__ __forceinline__ void kv_cap(V (&s)[N], const AttnArgs& p) {
+__device__ __forceinline__ void kv_cap(V (&s)[N], const AttnMore& p) {
     if (BF16 && kv_near(p)) kv_cap_near(s, p);
     else kv_cap_far(s, p);
 }

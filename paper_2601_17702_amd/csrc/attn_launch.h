@@ -23,11 +23,11 @@ constexpr bool s3_whole_tiles(int R, bool list, int64_t units, int64_t tokens) {
 // Sequences, or tiles of listed blocks, of few rows (R: the most that one has, 128 at most); tiles: how many there can be;
 // most_tokens: a bound of what one sees.
 size_t s3_attn_stream_workspace(const s3_kv_cache* c, bool list, int R, int64_t units, int64_t most_tokens);
-int s3_attn_stream(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
+int s3_attn_stream(const s3_kv_cache* c, const AttnMore& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
 // Its builds for capped scores, for 8-bit caches (dtype kS3E4m3), and for both.
-int s3_attn_stream_cap(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
-int s3_attn_stream_8(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
-int s3_attn_stream_8_cap(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
+int s3_attn_stream_cap(const s3_kv_cache* c, const AttnMore& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
+int s3_attn_stream_8(const s3_kv_cache* c, const AttnMore& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
+int s3_attn_stream_8_cap(const s3_kv_cache* c, const AttnMore& p, int64_t tiles, int R, int64_t most_tokens, void* ws, hipStream_t st);
 
 // Chunks, or tiles of listed blocks, of more rows: row tiles of s3_attn_tile_rows rows, the tokens of each in n_split parts.
 int s3_attn_tile_rows(const s3_kv_cache* c);
@@ -36,9 +36,9 @@ size_t s3_attn_tile_workspace(const s3_kv_cache* c, int64_t units, int n_split);
 struct TileArgs {
     float* slots;             // partial sums where n_split > 1
     int n_split, tiles;       // row tiles that there can be
-    bool small;               // of 128 rows, where a call's other tiles would have 256
 };
-int s3_attn_tile(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int n_split, bool small, void* ws, hipStream_t st);
+static_assert(sizeof(AttnArgs) + sizeof(TileArgs) <= 176, "arguments of the builds without caps over bf16 and fp32: see AttnMore");
+int s3_attn_tile(const s3_kv_cache* c, const AttnMore& p, int64_t tiles, int n_split, bool small, void* ws, hipStream_t st);      // small: of 128 rows, where a call's other tiles would have 256
 // Whether an uncut call of the builds for 8 bits and for caps takes tiles of 128 rows: where those of 256 would leave half of the 256 compute
 // units idle. Dim 128, 8 heads with 4 query heads each, one sequence, tiles of 256 rows against tiles of 128, in us: 64 tokens of e4m3 11
 // against 9, 256 17 against 15, 512 24 against 22, 1024 (128 units) 39 against 38; with bf16 and a cap 12 against 9, 19 against 16, 28
@@ -47,6 +47,6 @@ constexpr bool s3_has_small_tiles(bool eight, bool bf16, int d_head, bool cap) {
 constexpr bool s3_small_tiles(bool eight, bool bf16, int d_head, bool cap, int64_t units, int n_split) {
     return s3_has_small_tiles(eight, bf16, d_head, cap) && n_split == 1 && units <= 128;
 }
-int s3_attn_tile_cap(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);
-int s3_attn_tile_8(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);
-int s3_attn_tile_8_cap(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st);
+int s3_attn_tile_cap(const s3_kv_cache* c, const AttnMore& p, const TileArgs& ta, bool small, hipStream_t st);
+int s3_attn_tile_8(const s3_kv_cache* c, const AttnMore& p, const TileArgs& ta, bool small, hipStream_t st);
+int s3_attn_tile_8_cap(const s3_kv_cache* c, const AttnMore& p, const TileArgs& ta, bool small, hipStream_t st);

@@ -39,9 +39,9 @@ size_t s3_attn_tile_workspace(const s3_kv_cache* c, int64_t units, int n_split) 
     return n_split > 1 ? s3_align((size_t)units * n_split * rows_of(c) * (c->d_head + 2) * 4) : 0;
 }
 
-int s3_attn_tile(const s3_kv_cache* c, const AttnArgs& p, int64_t tiles, int n_split, bool small, void* ws, hipStream_t st) {
-    const TileArgs ta{(float*)ws, n_split, (int)tiles, small};
-    if (c->dtype == kS3E4m3) return p.cap != 0.0f ? s3_attn_tile_8_cap(c, p, ta, st) : s3_attn_tile_8(c, p, ta, st);
-    if (p.cap != 0.0f) return s3_attn_tile_cap(c, p, ta, st);
-    return c->dtype == S3_BF16 ? launch_tile<__bf16, false>(c->d_head, p, ta, st) : launch_tile<float, false>(c->d_head, p, ta, st);
+int s3_attn_tile(const s3_kv_cache* c, const AttnMore& p, int64_t tiles, int n_split, bool small, void* ws, hipStream_t st) {
+    const TileArgs ta{(float*)ws, n_split, (int)tiles};
+    if (c->dtype == kS3E4m3) return p.cap != 0.0f ? s3_attn_tile_8_cap(c, p, ta, small, st) : s3_attn_tile_8(c, p, ta, small, st);
+    if (p.cap != 0.0f) return s3_attn_tile_cap(c, p, ta, small, st);
+    return c->dtype == S3_BF16 ? launch_tile<__bf16, false>(c->d_head, p, ta, small, st) : launch_tile<float, false>(c->d_head, p, ta, small, st);
 }

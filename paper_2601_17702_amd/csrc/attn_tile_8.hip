@@ -1,6 +1,6 @@
 // Attention of many rows over an 8-bit cache.
 #include "attn_tile_impl.inc"
 
-int s3_attn_tile_8(const s3_kv_cache* c, const AttnArgs& p, const TileArgs& ta, hipStream_t st) {
-    return launch_tile<kv_e4m3, false>(c->d_head, p, ta, st);
+int s3_attn_tile_8(const s3_kv_cache* c, const AttnMore& p, const TileArgs& ta, bool small, hipStream_t st) {
+    return launch_tile<kv_e4m3, false>(c->d_head, p, ta, small, st);
 }

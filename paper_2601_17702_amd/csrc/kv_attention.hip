@@ -69,7 +69,7 @@ struct Plan {
     }
 };
 
-int run(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b, AttnArgs p, Plan plan, void* ws, hipStream_t st) {
+int run(const char* fn, const s3_kv_cache* c, const s3_kv_batch* b, AttnMore p, Plan plan, void* ws, hipStream_t st) {
     const bool small = plan.many && s3_small_tiles(c->dtype == kS3E4m3, c->dtype != S3_FP32, c->d_head, p.cap != 0.0f, plan.many_tiles * c->n_kv_heads, plan.n_split);
     if (small) plan.cut(128);
     p.few = plan.few ? plan.limit : 0;
@@ -117,10 +117,10 @@ int attend(const Call& x, int window, const int32_t* sel, int q_block, int top_b
     if (int rc = check_ws(x.fn, x.ws, x.ws_bytes, plan.bytes())) return rc;
     const float log2e = 1.4426950408889634f;
     const bool cap = x.softcap > 0.0f, near = cap && c.dtype != S3_FP32 && x.softcap <= kS3NearCap;
-    const AttnArgs p{s3_kv_batch_args(&c, x.b), (const char*)x.q, (char*)x.out, x.lse, (const char*)c.k, (const char*)c.v, x.scale8, sel, x.q_ts * es,
-                     x.q_hs * es, c.n_kv_heads, plan.G, x.n_q, window, 0, top_b, 1, q_block ? (int)s3_block_tiles(x.b, q_block) : 0,
-                     near ? 2.0f * x.softcap * log2e : cap ? 1.0f : x.scale * log2e, cap ? x.softcap * log2e : 0.0f, cap ? x.scale / x.softcap : 0.0f,
-                     near ? x.softcap * log2e : 0.0f, 0};
+    const AttnMore p{{s3_kv_batch_args(&c, x.b), (const char*)x.q, (char*)x.out, x.lse, (const char*)c.k, (const char*)c.v, sel, x.q_ts * es, x.q_hs * es,
+                      c.n_kv_heads, plan.G, x.n_q, window, 0, top_b, 1, q_block ? (int)s3_block_tiles(x.b, q_block) : 0,
+                      near ? 2.0f * x.softcap * log2e : cap ? 1.0f : x.scale * log2e, 0},
+                     x.scale8, cap ? x.softcap * log2e : 0.0f, cap ? x.scale / x.softcap : 0.0f, near ? x.softcap * log2e : 0.0f};
     return run(x.fn, &c, x.b, p, plan, x.ws, (hipStream_t)x.stream);
 }
 int check_window(const char* fn, int window) { return window < 0 ? s3_fail(S3_EINVAL, "%s: window %d", fn, window) : S3_OK; }
