@@ -708,7 +708,8 @@ class KVCache:
 class KVCache8(KVCache):
     """The same in 8 bits (s3_kv8_cache): half of a bf16 cache's memory, and of its traffic.  k [n_pages, n_kv_heads, d_head / 16, page_size, 16] and
     v [n_pages, n_kv_heads, page_size / 16, d_head, 16] in float8_e4m3fn, scale [n_pages, n_kv_heads, 2, page_size] uint8: element times
-    2^(code - 127) is what it stands for.  Every call of KVCache is here, with the same arguments; rows are bfloat16."""
+    2^(code - 127) is what it stands for.  Every call of KVCache is here, with the same arguments; rows are bfloat16.  The argument `scale` takes those codes, which the cache
+    keeps as .codes; .scale is what attention multiplies scores by, as in KVCache."""
 
     _eight = True
 

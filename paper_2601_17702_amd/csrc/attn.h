@@ -42,7 +42,7 @@ struct AttnArgs {
     float sl;                 // scale * log2(e), or what capped scores are to be multiplied by
     int few;                  // sequences of at most this many rows are the streaming kernel's
 };
-// What 8-bit caches and caps need beside.  The other builds are launched without it: every argument is read from memory when a workgroup begins, and with these 0.1 to 0.7 us
+// What 8-bit caches and caps need beside.  The other builds are launched without it: every argument is read from memory when a workgroup begins, and with these 0.1 to 0.8 us
 // of a tiled call's two launches were lost (16 tokens at 20000, 28 heads over 4: 28.1 -> 28.8; 333 at 333 in fp32 with 256 channels: 37.6 -> 38.3).
 struct AttnMore : AttnArgs {
     const uint8_t* scale;     // an 8-bit cache's

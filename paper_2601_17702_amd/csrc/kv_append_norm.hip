@@ -3,12 +3,13 @@
 //   y = w x / sqrt(sum x^2 / d + eps)      the mean square in 64 bits, its root's inverse r rounded to fp32 once, (x r) and (x r) w to fp32
 //   rotation as in kv_append.hip, in fp32; then one rounding to the cache's type, or with 8 bits
 //   code c = the smallest that leaves max|x| 2^(127 - c) <= 448, element = e4m3(x 2^(127 - c)), to nearest even
-// A power of two as a scale costs no precision (e4m3 values have the same 4 bits in every octave of 17) and makes both scalings exact.
+// A power of two makes both scalings exact.  e4m3 values have 4 bits in 15 octaves and 3, 2 and 1 in the three below: elements down to 1/14336 of the row's largest keep all 4, where
+// max/448 as a scale would take up to an octave more.
 //
 // What bounds it: memory.  A row of d channels lies in d / 16 lanes, 16 channels each: where pairs are (i, i + rot / 2) eight of one half and
 // their eight partners, so a rotation needs no other lane's channels, and a norm's sum is exchanged between neighbours of a row of 16 lanes only.  Two rows' loads are under way
-// in a thread before the first is worked on.  Eight chunks of 2048 tokens into 8 bits, 32 query heads over 8 of 128 (387 MB): 82 to 85 us, 4.6 TB/s; 116 with 8 channels a
-// lane and no loads ahead, 134 with 16 and none, 86 with four rows'.  64 single tokens: 6.7 us, a chain of loads.
+// in a thread before the first is worked on.  Eight chunks of 2048 tokens into 8 bits, 32 query heads over 8 of 128 (379 MB): 83 to 85 us, 4.5 TB/s; 116 with 8 channels a
+// lane and no loads ahead, 134 with 16 and none, 86 with four rows'.  64 single tokens: 7.1 us, a chain of loads.
 #include "kv_cache.h"
 
 namespace {
