@@ -408,8 +408,9 @@ int s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const void*
  * within 2^-8 of the weighted sum of magnitudes, and once more 2^-8 of themselves by their own rounding.
  *   q    [n_tokens][n_q_heads][d_head], strides as in s3_kv_append;  out [n_tokens][n_q_heads][d_head] contiguous, dtype
  *   ws   s3_paged_attention_workspace(...) bytes, 256-byte aligned, contents meaningless between calls.  The size is this call's: a smaller batch, which is cut into
- *        more parts, may take more.  Where max_new * G <= 32 (lists: min(max_new, q_block) * G) no batch takes more than one of a single sequence with n_tokens = max_new
- *        and the same max_kv (top_b), so that a buffer of that size is enough for all of them; with longer chunks ask before every call
+ *        more parts, may take more.  Where max_new * G <= 32 no batch takes more than one of a single sequence with n_tokens = max_new and the same max_kv, and of lists where
+ *        t = min(max_new, q_block) has t * G <= 32 none more than one sequence with n_tokens = max_new = t and the same top_b: a buffer of that size is enough for all of them.
+ *        With longer chunks ask before every call
  * Limits: 1 <= G <= 32; scale > 0; window >= 0.  n_kv_heads times n_seq below 2^22, and times the chunks' tiles of 128 rows (n_tokens * G / 128,
  * one more for every sequence of more than 32 rows). */
 size_t s3_paged_attention_workspace(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_q_heads);

@@ -30,11 +30,29 @@ def test_no_access_is_wider_than_what_callers_align():
 
 @pytest.mark.parametrize("dtype", [s3.S3_BF16, s3.S3_FP32, "e4m3"])
 @pytest.mark.parametrize("d,heads,G", [(64, 1, 1), (128, 8, 4), (256, 2, 7), (128, 3, 16), (64, 4, 32), (256, 64, 2)])
+def test_scratch_of_one_tile_is_enough_for_any_lists_of_few_rows(dtype, d, heads, G):
+    """Of listed blocks the batch that takes most is one tile of queries, whatever the chunks' lengths."""
+    L = s3.lib()
+    c = cache8(heads=heads, d=d) if dtype == "e4m3" else cache16(heads=heads, d=d, dtype=dtype)
+    need = L.s3_kv8_block_attention_workspace if dtype == "e4m3" else L.s3_block_attention_workspace
+    for q_block in {1, 2, 32 // G, 64}:
+        for max_new in (1, 2, 5, 64, 1000):
+            t = min(max_new, q_block)
+            if t < 1 or t * G > 32:
+                continue
+            for top in (1, 16, 17, 128, 129, 4096):
+                one = need(c, batch(n_seq=1, n_tokens=t, max_new=t), heads * G, q_block, top)
+                for n_seq, n_tokens in ((1, 1), (1, t), (1, max_new), (2, 1), (2, max_new + 1), (3, 3 * max_new), (40, 40), (40, 40 * max_new), (300, 300 * max_new)):
+                    assert need(c, batch(n_seq=n_seq, n_tokens=n_tokens, max_new=max_new), heads * G, q_block, top) <= one, (q_block, max_new, top, n_seq, n_tokens)
+
+
+@pytest.mark.parametrize("dtype", [s3.S3_BF16, s3.S3_FP32, "e4m3"])
+@pytest.mark.parametrize("d,heads,G", [(64, 1, 1), (128, 8, 4), (256, 2, 7), (128, 3, 16), (64, 4, 32), (256, 64, 2)])
 def test_scratch_of_one_sequence_is_enough_for_any_batch_of_few_rows(dtype, d, heads, G):
     """A buffer that a program keeps while sequences come and go: sized for one sequence, it holds for every number of them, and for shorter bounds than its own."""
     L = s3.lib()
     c = cache8(heads=heads, d=d) if dtype == "e4m3" else cache16(heads=heads, d=d, dtype=dtype)
-    all_of, lists = (L.s3_kv8_attention_workspace, L.s3_kv8_block_attention_workspace) if dtype == "e4m3" else (L.s3_paged_attention_workspace, L.s3_block_attention_workspace)
+    all_of = L.s3_kv8_attention_workspace if dtype == "e4m3" else L.s3_paged_attention_workspace
 
     def many(n_seq, max_new, max_kv):
         pages = -(-max_kv // 64)
@@ -50,6 +68,4 @@ def test_scratch_of_one_sequence_is_enough_for_any_batch_of_few_rows(dtype, d, h
                 seen.add(need == one)
                 assert need <= one, (max_new, max_kv, n_seq)
                 assert all_of(c, many(n_seq, max_new, max(1, max_kv // 3)), heads * G) <= one
-                for q_block, top in ((1, 1), (1, 16), (1, 17), (max_new, 128), (max_new, 129), (64, 500)):
-                    assert lists(c, many(n_seq, max_new, max_kv), heads * G, q_block, top) <= lists(c, many(1, max_new, max_kv), heads * G, q_block, top)
     assert seen == {True, False} if dtype == "e4m3" and G < 32 else seen == {True}      # over 8 bits there are batches that need none
